@@ -319,6 +319,140 @@ int mita_attend(const mita_cfg_t *cfg, const void *q, const void *q_lm, const vo
 int mita_backward(const mita_cfg_t *cfg, const void *q, const void *k, const void *v, const void *o,
                   const void *dO, void *dq, void *dk, void *dv, void *ws, size_t ws_bytes, mita_stream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Dense attention: the softmax attention that MiTA stands in for (Sec. 3.2
+ * compares with it; a model may keep some of its layers dense), with grouped
+ * heads, lengths and windows, its backward pass, and the layer norm of tokens,
+ * queries and keys around either attention.
+ *
+ * The conventions above hold (device pointers, streams, errors, workspace),
+ * except that tensors may be strided.
+ * ------------------------------------------------------------------------ */
+
+/* Longest query or key sequence of the dense attention. */
+#define MITA_DENSE_MAX_N (1 << 20)
+/* Largest distance between two tokens of one head, in elements. */
+#define MITA_DENSE_MAX_STRIDE (1 << 22)
+
+/* Distances between batch elements, heads and tokens of a [B, H, N, d] tensor
+ * in elements; the d elements of a token are consecutive. All zero: contiguous
+ * [B, H, N, d]. [B, N, H, d] and the slices of a fused projection
+ * [B, N, 3, H, d] are other uses. Every distance is a multiple of 16 bytes. */
+typedef struct {
+  int64_t b, h, n;
+} mita_strides_t;
+
+/*
+ * Dense attention problem. Query head h reads key head h / (H / H_kv). With
+ * lengths (below) batch element b holds q_len[b] queries and k_len[b] keys,
+ * else N and N_k; a sequence's last query stands at its last key: query i has
+ * position p = i + k_len - q_len, and sees the keys j of its sequence with
+ * p - left <= j <= p + right (left, right = -1: no bound; right = 0: causal).
+ */
+typedef struct {
+  int32_t B, H, H_kv;      /* batch, query heads, key/value heads; H_kv divides H */
+  int32_t N, N_k, d;       /* queries, keys (each in [1, MITA_DENSE_MAX_N]), head dim in {64, 128} */
+  int32_t dtype;           /* MITA_F32 or MITA_BF16: storage of all tensors but the log-sum-exps */
+  int32_t left, right;     /* window, -1 for no bound */
+  float scale;             /* softmax scale; 0 means 1/sqrt(d) */
+  mita_strides_t q, k, v, o;        /* inputs may repeat batch elements or heads (distance 0) */
+  mita_strides_t dO, dq, dk, dv;    /* of the backward pass */
+} mita_dense_cfg_t;
+
+/* Host-only validation of cfg; a status code. */
+int mita_dense_check(const mita_dense_cfg_t *cfg);
+
+/* Bytes of workspace mita_dense_forward (which = MITA_WS_FORWARD) or
+ * mita_dense_backward (MITA_WS_BACKWARD) needs (0 if cfg is invalid). It
+ * depends on the sizes, the type and the window, not on the strides. */
+size_t mita_dense_workspace_size(const mita_dense_cfg_t *cfg, int which);
+
+/*
+ * o_i = sum_j softmax_j(scale q_i . k_j) v_j over the keys that query i sees,
+ * and lse_i = log sum_j exp(scale q_i . k_j) (natural logarithm).
+ *   q, o : [B, H, N, d];  k, v : [B, H_kv, N_k, d] by cfg's strides; o must
+ *          not overlap an input;
+ *   q_len, k_len : [B] int32 lengths in [0, N] and [0, N_k] (values outside
+ *          are clamped), or NULL; what lies behind a sequence's end is not
+ *          used and may hold anything;
+ *   lse  : [B, H, N] fp32 contiguous output, or NULL;
+ *   ws   : >= mita_dense_workspace_size(cfg, MITA_WS_FORWARD) bytes.
+ * A query that sees no key, and every query behind its sequence's end, gets
+ * o = 0 and lse = -infinity. Values a window hides must be finite (NaN or
+ * infinite inputs inside a sequence are a caller error, as everywhere).
+ * Scores, softmax and sums are fp32; in bf16 the weights are rounded once to
+ * bf16 to multiply v. Results are the same bit for bit from call to call.
+ * A few queries against many keys (single tokens) are split over the keys.
+ */
+int mita_dense_forward(const mita_dense_cfg_t *cfg, const void *q, const void *k, const void *v, const int32_t *q_len,
+                       const int32_t *k_len, void *o, float *lse, void *ws, size_t ws_bytes, mita_stream_t stream);
+
+/*
+ * Gradients of mita_dense_forward's o for an upstream gradient dO, from its
+ * inputs and outputs: P_ij = exp(scale q_i . k_j - lse_i) is formed again,
+ * D_i = dO_i . o_i, dS = P (dO v^T - D), dq = scale dS k, dk = scale dS^T q,
+ * dv = P^T dO, the key side summed over the query heads of each key head.
+ *   q, k, v, q_len, k_len : the forward's;  o, lse : its outputs;
+ *   dO, dq : [B, H, N, d];  dk, dv : [B, H_kv, N_k, d] by cfg's strides; the
+ *          gradients must not overlap the inputs or each other;
+ *   ws   : >= mita_dense_workspace_size(cfg, MITA_WS_BACKWARD) bytes.
+ * Every element of dq, dk and dv is written: queries and keys behind their
+ * sequence's end get 0. An input that repeats batch elements or heads (distance
+ * 0) still gets one gradient for each of them. No atomics: results are the
+ * same bit for bit from call to call.
+ */
+int mita_dense_backward(const mita_dense_cfg_t *cfg, const void *q, const void *k, const void *v, const void *o,
+                        const float *lse, const void *dO, const int32_t *q_len, const int32_t *k_len, void *dq,
+                        void *dk, void *dv, void *ws, size_t ws_bytes, mita_stream_t stream);
+
+/* Widest row of the layer norm. */
+#define MITA_NORM_MAX_C 65536
+
+/*
+ * Layer norm over the C elements of each row of an [n[0], n[1], n[2], C]
+ * tensor (tokens: n = {1, 1, tokens}; queries or keys of every head: {B, H, N}).
+ * x, y, dy and dx each have their distances between rows, in elements; all
+ * zero: contiguous. Any element alignment is accepted; rows whose addresses
+ * and widths are multiples of 16 bytes are read and written 16 bytes at a time.
+ */
+typedef struct {
+  int32_t n[3], C;         /* rows, 1 <= C <= MITA_NORM_MAX_C */
+  int32_t dtype;           /* MITA_F32 or MITA_BF16: x, y, dy, dx */
+  int32_t wdtype;          /* MITA_F32 or MITA_BF16: w, b, dw, db */
+  float eps;               /* > 0 */
+  int64_t x[3], y[3], dy[3], dx[3];
+} mita_norm_cfg_t;
+
+/* Host-only validation of cfg; a status code. */
+int mita_norm_check(const mita_norm_cfg_t *cfg);
+
+/* Bytes of workspace mita_norm_backward needs when dw or db is asked for (0 if
+ * cfg is invalid); mita_norm_forward needs none. */
+size_t mita_norm_workspace_size(const mita_norm_cfg_t *cfg);
+
+/*
+ * y = (x - mean) rstd w + b per row, rstd = 1 / sqrt(variance + eps) with the
+ * variance about the row's mean (divided by C), all in fp32.
+ *   w, b : [C], or NULL (1 and 0);  mean, rstd : [n0, n1, n2] fp32 contiguous
+ *   outputs for the backward pass, or NULL. y may be x with the same strides,
+ *   and must not overlap it otherwise.
+ */
+int mita_norm_forward(const mita_norm_cfg_t *cfg, const void *x, const void *w, const void *b, void *y, float *mean,
+                      float *rstd, mita_stream_t stream);
+
+/*
+ * With h = (x - mean) rstd and g = dy w: dx = rstd (g - mean(g) - h mean(g h))
+ * per row, dw = sum over rows of dy h, db = sum over rows of dy. The row sums
+ * are added in a fixed order in fp32 (the same bit for bit from call to call)
+ * and rounded once.
+ *   mean, rstd : the forward's;  w : the forward's, or NULL;
+ *   dx : output or NULL;  dw, db : [C] outputs, each may be NULL. dx may be dy
+ *   with the same strides, and must not overlap it or x otherwise;
+ *   ws : >= mita_norm_workspace_size(cfg) bytes if dw or db is given.
+ */
+int mita_norm_backward(const mita_norm_cfg_t *cfg, const void *x, const void *w, const float *mean, const float *rstd,
+                       const void *dy, void *dx, void *dw, void *db, void *ws, size_t ws_bytes, mita_stream_t stream);
+
 /*
  * Per-launch timing of mita_forward with HIP events (profiling aid).
  * A timer holds event slots for up to max_calls forward calls. Each

@@ -21,19 +21,26 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmita.so")
 ARCH = "gfx950"
 
-SOURCES = ["mita_api.hip", "pool_scores.hip", "topk.hip", "select.hip", "route_attend.hip", "backward.hip", "tome.hip"]
+SOURCES = ["mita_api.hip", "pool_scores.hip", "topk.hip", "select.hip", "route_attend.hip", "backward.hip", "tome.hip",
+           "dense_forward.hip", "dense_backward.hip", "norm.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-fPIC", "-std=c++17",
     # no packed fp32 arithmetic in device code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # MFMA accumulators in ordinary VGPRs: no copies between AGPRs and VGPRs
-    # around the VALU work on the same values
-    "-Xarch_device", "-mllvm=-amdgpu-mfma-vgpr-form=1",
     "-I", os.path.join(ROOT, "include"),
     "-Wno-unused-command-line-argument",
 ]
+# MFMA accumulators in ordinary VGPRs: no copies between AGPRs and VGPRs around
+# the VALU work on the same values. Not for the dense attention: kernels of two
+# waves per SIMD get that form anyway, and in the fp32 ones, which hold more than
+# 256 registers, the forced form lost accumulators (dQ at d = 128 off by 5%).
+VGPR_FORM = ["-Xarch_device", "-mllvm=-amdgpu-mfma-vgpr-form=1"]
+
+
+def flags_for(src):
+    return FLAGS if src.startswith("dense_") else FLAGS + VGPR_FORM
 
 
 def _run(cmd):
@@ -50,7 +57,7 @@ def build(jobs: int | None = None, verbose: bool = False) -> str:
 
     def compile_one(src):
         obj = os.path.join(BUILD, src.replace(".hip", ".o"))
-        cmd = [HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [HIPCC, *flags_for(src), "-c", os.path.join(CSRC, src), "-o", obj]
         rc, out = _run(cmd)
         if rc != 0:
             raise RuntimeError(f"hipcc failed on {src}:\n{out}")

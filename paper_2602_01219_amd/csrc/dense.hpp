@@ -1,0 +1,327 @@
+// dense.hpp - building blocks of the dense attention kernels: row tiles staged
+// in LDS, 32x32 MFMA products of a tile with operands held in registers, and the
+// block order.
+//
+// A wave owns 32 columns (query rows in the forward and the query side of the
+// backward, keys in its key side); lane l = 32 g + n belongs to column n. A tile
+// holds 32 or 64 rows of D elements (keys and values, or queries and their
+// gradients). Two products are formed with it:
+//   rows:  C[i][n] = sum_d X[i][d] B[d][n]     (32 tile rows by 32 columns; B in registers)
+//   cols:  A[d][n] += sum_i X[i][d] P[i][n]    (P as it left a `rows` product)
+// A v_mfma_f32_32x32 accumulator holds C[8 (i / 4) + 4 g + i % 4][n], i = 0..15.
+// As the B operand of the next product a lane needs rows of its own group g, and
+// which rows a group takes is free as long as both operands agree: the
+// accumulator's own rows serve, so P never moves between lanes.
+// bf16: one v_mfma_f32_32x32x16_bf16 per 16-long reduction step; fp32: four
+// v_mfma_f32_32x32x2_f32 per 8-long step, so both types read 16 bytes of a row
+// (chunk 2 s + g of step s) per lane for the `rows` product.
+#pragma once
+#include "cdna4.hpp"
+#include "flash.hpp"
+
+namespace mita {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+__device__ __forceinline__ f32x16 splat16(float x) {
+  return f32x16{x, x, x, x, x, x, x, x, x, x, x, x, x, x, x, x};
+}
+// The tile row of accumulator element i for lane group g.
+__device__ __forceinline__ int acc_row(int i, int g) { return 8 * (i >> 2) + 4 * g + (i & 3); }
+
+template <typename T, int D> struct RowTile {
+  static constexpr int RB = D * (int)sizeof(T);  // bytes per row
+  static constexpr int CPR = RB / 16;            // 16-byte chunks per row
+  static constexpr int RPI = 64 / CPR;           // rows one wave-wide copy fills
+  static constexpr int NS = CPR / 2;             // reduction steps of a `rows` product
+  static constexpr int NB = D / 32;              // 32-wide blocks of d
+  static constexpr int TR = sizeof(T) == 2 ? 64 : 32;  // rows per staged tile
+  // Slot s of row r holds chunk s ^ swz(r). LDS serves 256 bytes per cycle: 16
+  // lanes of the 16-byte reads (16 consecutive rows at one chunk), 32 lanes of
+  // the transposing 8-byte reads (4 rows by 4 chunks), 64 lanes of fp32's 4-byte
+  // reads (8 chunks of two rows 4 apart). With these each falls into 16
+  // different 16-byte columns.
+  __device__ __forceinline__ static int swz(int r) {
+    if (sizeof(T) == 4) return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3);
+    if (CPR == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+    return (r & 3) << 2 | ((r >> 2) & 3);
+  }
+};
+
+// LDS DMA of 16 (4) bytes per lane: lane l's go to dst + 16 l (4 l).
+__device__ __forceinline__ void copy16(const void *src, char *dst) {
+  __builtin_amdgcn_global_load_lds(src, (lds_void_t *)dst, 16, 0, 0);
+}
+__device__ __forceinline__ void copy4(const void *src, char *dst) {
+  __builtin_amdgcn_global_load_lds(src, (lds_void_t *)dst, 4, 0, 0);
+}
+
+// The copies this wave issued have landed, and those of every wave once all are
+// here. (The barrier alone does not wait for them: a wave that reads none of the
+// tile, or reads it behind the barrier, would pass with its own in flight.)
+__device__ __forceinline__ void tile_barrier() {
+  wait_loads();
+  __syncthreads();
+}
+
+// A tile's copy into LDS by DMA (global_load_lds_dwordx4), NW waves: lane l of
+// copy `ins` fills slot l % CPR of row ins * RPI + l / CPR.
+template <typename T, int D, int NW> struct TileCopy {
+  using RT = RowTile<T, D>;
+  static constexpr int PW = RT::TR / RT::RPI / NW;  // copies per wave
+  static_assert(PW >= 1 && RT::TR % (RT::RPI * NW) == 0, "whole copies per wave");
+  int w;               // the wave, as a scalar
+  uint32_t row[PW];    // the lane's row of each copy
+  uint32_t chunk[PW];  // byte offset of its chunk in the row
+  uint32_t off[PW];    // row * stride + chunk, for whole tiles
+  __device__ __forceinline__ void init(uint32_t stride) {
+    w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < PW; ++j) {
+      const int r = (w * PW + j) * RT::RPI + lane / RT::CPR;
+      row[j] = (uint32_t)r;
+      chunk[j] = (uint32_t)(((lane % RT::CPR) ^ RT::swz(r)) << 4);
+      off[j] = row[j] * stride + chunk[j];
+    }
+  }
+  // rows `first` .. of a matrix whose rows are `stride` bytes apart; of the tile's
+  // rows only the first nrows (>= 1) exist, the others repeat the last of them
+  __device__ __forceinline__ void issue(char *tile, const char *base, int64_t first, uint32_t stride,
+                                        int nrows) const {
+    const char *src = base + first * (int64_t)stride;
+#pragma unroll
+    for (int j = 0; j < PW; ++j) {
+      const uint32_t o = nrows >= RT::TR ? off[j] : min(row[j], (uint32_t)(nrows - 1)) * stride + chunk[j];
+      copy16(src + o, tile + (w * PW + j) * 1024);
+    }
+  }
+};
+
+// Per-lane LDS addresses of the two products, fixed for every tile.
+template <typename T, int D> struct TileAddr {
+  using RT = RowTile<T, D>;
+  uint32_t r0;                                     // `rows`: chunk g of row n; step s is r0 ^ (s << 5)
+  uint32_t c[sizeof(T) == 2 ? 2 * RT::NB : 1];     // `cols`, see tile_cols
+  __device__ __forceinline__ void init() {
+    const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
+    r0 = (uint32_t)(n * RT::RB + ((g ^ RT::swz(n)) << 4));
+    if constexpr (sizeof(T) == 2) {
+      // 16-lane groups read 4 x 16 blocks transposed (ds_read_b64_tr_b16: lane
+      // 4 e + p addresses piece p of row e, lane i receives column i): rows
+      // 8 h + 4 g + e, columns 32 db + 16 ((lane >> 4) & 1) + i
+      const int e = (lane & 15) >> 2, p = lane & 3, half = (lane >> 4) & 1;
+#pragma unroll
+      for (int db = 0; db < RT::NB; ++db)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = 8 * h + 4 * g + e;
+          c[2 * db + h] = (uint32_t)(r * RT::RB + (((4 * db + 2 * half + (p >> 1)) ^ RT::swz(r)) << 4) + ((p & 1) << 3));
+          pin(c[2 * db + h]);
+        }
+    } else {
+      // row 8 q + 4 g + r, element n of block db: c ^ (db << 7) ^ swizzle(q, r), + (8 q + r) rows
+      c[0] = (uint32_t)(4 * g * RT::RB + (((n >> 2) ^ (g << 3)) << 4) + ((n & 3) << 2));
+    }
+  }
+};
+
+// One reduction step of a `rows` product.
+__device__ __forceinline__ f32x16 mma32(bf16_t *, const uint4 &a, const uint4 &b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                 0);
+}
+__device__ __forceinline__ f32x16 mma32(float *, const uint4 &a, const uint4 &b, f32x16 c) {
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+}
+
+// c + X B for the 32 tile rows from 32 kb on.
+template <typename T, int D>
+__device__ __forceinline__ f32x16 tile_rows(const char *tile, const TileAddr<T, D> &ad, int kb,
+                                            const uint4 (&b)[RowTile<T, D>::NS], f32x16 c) {
+  using RT = RowTile<T, D>;
+#pragma unroll
+  for (int s = 0; s < RT::NS; ++s) {
+    const uint4 a = *reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)(s << 5)) + kb * 32 * RT::RB);
+    c = mma32((T *)nullptr, a, b[s], c);
+  }
+  return c;
+}
+
+// P as the B operand: bf16 rounds it (16 rows per operand), fp32 takes it as it is.
+template <typename T> struct ColsOperand;
+template <> struct ColsOperand<bf16_t> {
+  uint4 b[2];
+  __device__ __forceinline__ explicit ColsOperand(const f32x16 &p) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      b[s] = make_uint4(pack_bf16x2(p[8 * s], p[8 * s + 1]), pack_bf16x2(p[8 * s + 2], p[8 * s + 3]),
+                        pack_bf16x2(p[8 * s + 4], p[8 * s + 5]), pack_bf16x2(p[8 * s + 6], p[8 * s + 7]));
+  }
+};
+template <> struct ColsOperand<float> {
+  f32x16 p;
+  __device__ __forceinline__ explicit ColsOperand(const f32x16 &x) : p(x) {}
+};
+
+// acc[db] += X^T P for the 32 tile rows from 32 kb on.
+template <int D>
+__device__ __forceinline__ void tile_cols(f32x16 (&acc)[D / 32], const char *tile, const TileAddr<bf16_t, D> &ad, int kb,
+                                          const ColsOperand<bf16_t> &P) {
+  using RT = RowTile<bf16_t, D>;
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int db = 0; db < RT::NB; ++db) {
+      uint2 h[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        h[i] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                             (lds_v4i16_t *)(tile + ad.c[2 * db + i] + (32 * kb + 16 * s) * RT::RB)));
+      acc[db] = mma32((bf16_t *)nullptr, make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), P.b[s], acc[db]);
+    }
+}
+template <int D>
+__device__ __forceinline__ void tile_cols(f32x16 (&acc)[D / 32], const char *tile, const TileAddr<float, D> &ad, int kb,
+                                          const ColsOperand<float> &P) {
+  using RT = RowTile<float, D>;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int q = i >> 2, r = i & 3;
+    const uint32_t at = ad.c[0] ^ (uint32_t)(((q & 1) << 2 | r) << 4);
+#pragma unroll
+    for (int db = 0; db < RT::NB; ++db) {
+      const float a =
+          *reinterpret_cast<const float *>(tile + (at ^ (uint32_t)(db << 7)) + (32 * kb + 8 * q + r) * RT::RB);
+      acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, P.p[i], acc[db], 0, 0, 0);
+    }
+  }
+}
+
+template <typename T, int D> using Column = uint4[RowTile<T, D>::NS];
+
+// The registers of a lane's column as B operand: the 16-byte chunks 2 s + g of
+// its row, zero without one.
+template <typename T, int D>
+__device__ __forceinline__ void load_column(Column<T, D> &b, const char *row, bool valid) {
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int s = 0; s < RowTile<T, D>::NS; ++s)
+    b[s] = valid ? *reinterpret_cast<const uint4 *>(row + 32 * s + 16 * g) : make_uint4(0, 0, 0, 0);
+}
+
+// The column's accumulators (d = 32 db + acc_row(i, g)) times `mul` to its row,
+// 16 bytes per lane and store: bf16 lanes n and n + 32 exchange half of their
+// 4-wide pieces, so each holds 8 consecutive elements.
+template <int D>
+__device__ __forceinline__ void store_column(float *row, const f32x16 (&acc)[D / 32], float mul, bool valid) {
+  const int g = (threadIdx.x & 63) >> 5;
+  if (!valid) return;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<float4 *>(row + 32 * db + 8 * q + 4 * g) = make_float4(
+          acc[db][4 * q] * mul, acc[db][4 * q + 1] * mul, acc[db][4 * q + 2] * mul, acc[db][4 * q + 3] * mul);
+}
+template <int D>
+__device__ __forceinline__ void store_column(bf16_t *row, const f32x16 (&acc)[D / 32], float mul, bool valid) {
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; q += 2) {
+      uint32_t x[2], y[2];  // pieces q and q + 1
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[i] = pack_bf16x2(acc[db][4 * q + 2 * i] * mul, acc[db][4 * q + 2 * i + 1] * mul);
+        y[i] = pack_bf16x2(acc[db][4 * q + 4 + 2 * i] * mul, acc[db][4 * q + 5 + 2 * i] * mul);
+      }
+      // first: piece q of the low half's lanes, q + 1 of the low half's in the
+      // high lanes; second: the high half's
+      const auto a = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
+      const auto b = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
+      if (valid) *reinterpret_cast<uint4 *>(row + 32 * db + 8 * (q + g)) = make_uint4(a[0], b[0], a[1], b[1]);
+    }
+}
+
+// Sum (maximum) of x over the two lanes of a column.
+__device__ __forceinline__ float column_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ __forceinline__ float column_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// ---------------------------------------------------------------------------
+// Arguments and index arithmetic
+// ---------------------------------------------------------------------------
+struct DenseMat {
+  const char *p;
+  int64_t b, h;  // bytes between batch elements and heads
+  uint32_t n;    // bytes between tokens
+};
+struct DenseArgs {
+  DenseMat q, k, v, o, dO;        // o is written by the forward
+  DenseMat dq, dk, dv;            // written
+  const int32_t *q_len, *k_len;
+  float *lse;                     // [B, H, N], written by the forward; may be NULL there
+  float *part_o, *part_lse;       // the forward's splits
+  float *row_lse, *row_D;         // the backward's rows (log2 units; see dense_backward.hip), padded to tiles
+  float *part_q, *part_k, *part_v;
+  int B, H, Hkv, G, N, Nk, R;
+  int left, right;
+  uint64_t magic;                 // 2^40 / G + 1
+  float scale, sl2;               // sl2 = scale * log2(e)
+  int tiles, splits;
+};
+
+// r / G for r < 2^27, G <= 2^12: r * (2^40 / G + 1) errs by less than r / 2^40
+// of a quotient step, below 1 / G
+__device__ __forceinline__ int div_group(const DenseArgs &a, int r) {
+  return (int)(((uint64_t)(uint32_t)r * a.magic) >> 40);
+}
+
+struct DenseSlice {
+  int b, hk, qlen, klen, off;  // off: position of query 0
+};
+__device__ __forceinline__ DenseSlice dense_slice(const DenseArgs &a, int s) {
+  DenseSlice x;
+  x.b = s / a.Hkv;
+  x.hk = s - x.b * a.Hkv;
+  x.qlen = a.q_len ? min(max(a.q_len[x.b], 0), a.N) : a.N;
+  x.klen = a.k_len ? min(max(a.k_len[x.b], 0), a.Nk) : a.Nk;
+  x.off = x.klen - x.qlen;
+  return x;
+}
+// Keys [lo, hi) that query `tok` sees (hi <= lo: none).
+__device__ __forceinline__ int first_key(const DenseArgs &a, const DenseSlice &x, int tok) {
+  return max(0, tok + x.off - a.left);
+}
+__device__ __forceinline__ int end_key(const DenseArgs &a, const DenseSlice &x, int tok) {
+  return min(x.klen, tok + x.off + a.right + 1);
+}
+
+// Block id -> (slice, work item of the slice). Consecutive ids go to the eight
+// XCDs in turn; a slice's items stay on one XCD, whose L2 then holds the rows
+// they share, except for the last S % 8 slices, whose items go round all XCDs.
+__device__ __forceinline__ void dense_block(int id, int S, int items, int &slice, int &item) {
+  const int whole = S & ~7;
+  if (id < whole * items) {
+    const int j = id >> 3;
+    slice = (id & 7) + 8 * (j / items);
+    item = j % items;
+  } else {
+    const int j = id - whole * items, rest = S - whole;
+    // items outermost: the heavy first items of every slice start first
+    slice = whole + j % rest;
+    item = j / rest;
+  }
+}
+
+}  // namespace mita

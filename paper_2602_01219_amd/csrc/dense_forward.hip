@@ -1,0 +1,260 @@
+// dense_forward.hip - dense attention: o = softmax(scale Q K^T) V over the keys
+// each query sees, and the rows' log-sum-exps, with an online softmax.
+//
+// The query heads of one key head are rows of one matrix (row r: query r / G of
+// head r % G), so grouped heads share the staged keys, and one token of many
+// heads fills a tile.
+#include "dense.hpp"
+#include "kernels.hpp"
+#include "layer_check.hpp"
+
+namespace mita {
+
+// A wave's 32 rows: o^T accumulators, the reference -m of the weights exp2(z - m)
+// (log2 units), the raw dot above which the reference moves, and the lane's part
+// of the weight sum.
+template <int D> struct DenseState {
+  f32x16 o[D / 32];
+  float nm, thr, l;
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] = splat16(0.f);
+    nm = 0.f;
+    thr = -INFINITY;
+    l = 0.f;
+  }
+};
+
+// 32 keys of a staged tile (rows 32 kb ..): scores, online softmax, values. lo and
+// hi bound the column's visible keys, counted from the block's first.
+template <typename T, int D, bool MASKED>
+__device__ __forceinline__ void dense_step(DenseState<D> &st, const char *Kt, const char *Vt, const TileAddr<T, D> &ad,
+                                           int kb, const uint4 (&q)[RowTile<T, D>::NS], float sl2, int lo, int hi) {
+  f32x16 s = tile_rows<T, D>(Kt, ad, kb, q, splat16(0.f));
+  const int g = (threadIdx.x & 63) >> 5;
+  if (MASKED) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int j = acc_row(i, g);
+      s[i] = j >= lo && j < hi ? s[i] : -INFINITY;
+    }
+  }
+  float mx = s[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+  // the reference moves only where a score passes it by more than RESCALE_LOG2
+  // (and at the column's first visible key): any reference gives the same softmax
+  if (__ballot(mx > st.thr)) {
+    const float cm = column_max(mx);
+    const bool up = cm > st.thr;
+    const float m = up ? cm * sl2 : -st.nm;
+    const float alpha = st.thr == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-st.nm - m);
+    st.nm = -m;
+    st.thr = up ? (m + RESCALE_LOG2) * __builtin_amdgcn_rcpf(sl2) : st.thr;
+    st.l *= alpha;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) st.o[i] *= alpha;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], sl2, st.nm));
+    st.l += s[i];
+  }
+  tile_cols<D>(st.o, Vt, ad, kb, ColsOperand<T>(s));
+}
+
+// Bound by the MFMA and VALU issue of long sequences (per score 4 D flops against
+// one exp2, a quarter-rate instruction, and about three full-rate ones); by the
+// bytes of K and V for few rows, where `splits` workgroups share a tile's keys.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(DenseArgs a) {
+  using RT = RowTile<T, D>;
+  constexpr int TR = RT::TR;
+  __shared__ __align__(16) char lds0[2 * TR * RT::RB];
+  __shared__ __align__(16) char lds1[2 * TR * RT::RB];
+  int s, item;
+  dense_block(blockIdx.x, a.B * a.Hkv, a.tiles * a.splits, s, item);
+  const int sp = item % a.splits;
+  const int tile = a.tiles - 1 - item / a.splits;  // causal: the longest first
+  const DenseSlice x = dense_slice(a, s);
+  const int lane = threadIdx.x & 63, n = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+
+  // the lane's row
+  const int row = tile * DENSE_TQ + 32 * w + n;
+  const int tok = div_group(a, row), head = x.hk * a.G + row - tok * a.G;
+  const bool exists = row < a.R, valid = exists && tok < x.qlen;
+  uint4 q[RT::NS];
+  load_column<T, D>(q, a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
+  const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
+
+  // the keys of the block and of the wave
+  const int b0 = div_group(a, tile * DENSE_TQ);
+  const int b1 = min(div_group(a, min(tile * DENSE_TQ + DENSE_TQ, a.R) - 1), x.qlen - 1);
+  const int kbeg = first_key(a, x, b0), kend = b0 <= b1 ? end_key(a, x, b1) : 0;
+  const int nt = kend > kbeg ? (kend - kbeg + TR - 1) / TR : 0;
+  const int per = (nt + a.splits - 1) / a.splits;
+  const int t0 = sp * per, t1 = min(nt, t0 + per);
+  const int wr = tile * DENSE_TQ + 32 * w;
+  const int w0 = wr < a.R ? div_group(a, wr) : x.qlen;
+  const int w1 = min(div_group(a, min(wr + 32, a.R) - 1), x.qlen - 1);
+  const bool busy = w0 <= w1;
+  const int lo0 = first_key(a, x, w0), lo1 = first_key(a, x, w1), hi0 = end_key(a, x, w0), hi1 = end_key(a, x, w1);
+
+  TileAddr<T, D> ad;
+  ad.init();
+  TileCopy<T, D, 4> ck, cv;
+  ck.init(a.k.n);
+  cv.init(a.v.n);
+  const char *kb = a.k.p + x.b * a.k.b + x.hk * a.k.h, *vb = a.v.p + x.b * a.v.b + x.hk * a.v.h;
+  DenseState<D> st;
+  st.init();
+
+  auto issue = [&](int t, char *buf) {
+    const int k0 = kbeg + t * TR;
+    ck.issue(buf, kb, k0, a.k.n, x.klen - k0);
+    cv.issue(buf + TR * RT::RB, vb, k0, a.v.n, x.klen - k0);
+  };
+  auto compute = [&](int t, const char *buf) {
+    const int k0 = kbeg + t * TR;
+    if (!busy) return;
+#pragma unroll
+    for (int h = 0; h < TR / 32; ++h) {
+      const int kh = k0 + 32 * h;
+      if (kh >= hi1 || kh + 32 <= lo0) continue;
+      if (kh >= lo1 && kh + 32 <= hi0)
+        dense_step<T, D, false>(st, buf, buf + TR * RT::RB, ad, h, q, a.sl2, 0, 0);
+      else
+        dense_step<T, D, true>(st, buf, buf + TR * RT::RB, ad, h, q, a.sl2, lo - kh, hi - kh);
+    }
+  };
+  // two buffers as objects of their own: the compiler can tell the copies in
+  // flight from the tile being read
+  if (t0 < t1) issue(t0, lds0);
+  for (int t = t0; t < t1; t += 2) {
+    tile_barrier();
+    if (t + 1 < t1) issue(t + 1, lds1);
+    compute(t, lds0);
+    if (t + 1 >= t1) break;
+    tile_barrier();
+    if (t + 2 < t1) issue(t + 2, lds0);
+    compute(t + 1, lds1);
+  }
+
+  const float l = column_sum(st.l);
+  const bool some = valid && l > 0.f;
+  const float inv = some ? 1.f / l : 0.f;
+  if (!some) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) st.o[i] = splat16(0.f);
+  }
+  const float lse2 = some ? __builtin_amdgcn_logf(l) - st.nm : -INFINITY;
+  if (a.splits == 1) {
+    store_column<D>((T *)(a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n), st.o, inv, exists);
+    if (a.lse && exists && lane < 32) a.lse[((int64_t)x.b * a.H + head) * a.N + tok] = lse2 * 0.69314718055994531f;
+  } else {
+    const int64_t at = ((int64_t)s * a.R + row) * a.splits + sp;
+    store_column<D>(a.part_o + at * D, st.o, inv, exists);
+    if (exists && lane < 32) a.part_lse[at] = lse2;
+  }
+}
+
+// Joins a row's splits by their log-sum-exps: D / 4 lanes per row.
+template <typename T, int D> __global__ void __launch_bounds__(256) dense_join_kernel(DenseArgs a) {
+  constexpr int L = D / 4;
+  const int64_t i = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const int c = threadIdx.x % L;
+  if (i >= (int64_t)a.B * a.Hkv * a.R) return;
+  const int s = (int)(i / a.R), row = (int)(i - (int64_t)s * a.R);
+  const int b = s / a.Hkv, tok = div_group(a, row), head = (s - b * a.Hkv) * a.G + row - tok * a.G;
+  float m = -INFINITY;
+  for (int j = 0; j < a.splits; ++j) m = fmaxf(m, a.part_lse[i * a.splits + j]);
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int j = 0; j < a.splits; ++j) {
+    const float z = a.part_lse[i * a.splits + j];
+    if (z == -INFINITY) continue;  // no visible key in this split
+    const float f = __builtin_amdgcn_exp2f(z - m);
+    const float4 y = *reinterpret_cast<const float4 *>(a.part_o + (i * a.splits + j) * D + 4 * c);
+    l += f;
+    o.x += f * y.x;
+    o.y += f * y.y;
+    o.z += f * y.z;
+    o.w += f * y.w;
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  T *out = (T *)(a.o.p + b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n) + 4 * c;
+  out[0] = from_f32<T>(o.x * inv);
+  out[1] = from_f32<T>(o.y * inv);
+  out[2] = from_f32<T>(o.z * inv);
+  out[3] = from_f32<T>(o.w * inv);
+  if (a.lse && c == 0)
+    a.lse[((int64_t)b * a.H + head) * a.N + tok] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+}
+
+DenseArgs dense_args(const mita_dense_cfg_t &c) {
+  DenseArgs a{};
+  const size_t e = elem_bytes(c);
+  auto mat = [&](const mita_strides_t &s0, bool key) {
+    const mita_strides_t s = key ? strides_or(s0, c.H_kv, c.N_k, c.d) : strides_or(s0, c.H, c.N, c.d);
+    const int64_t n = key ? c.N_k : c.N;
+    return DenseMat{nullptr, s.b * (int64_t)e, s.h * (int64_t)e, n > 1 ? (uint32_t)(s.n * e) : 0u};
+  };
+  a.q = mat(c.q, false);
+  a.k = mat(c.k, true);
+  a.v = mat(c.v, true);
+  a.o = mat(c.o, false);
+  a.dO = mat(c.dO, false);
+  a.dq = mat(c.dq, false);
+  a.dk = mat(c.dk, true);
+  a.dv = mat(c.dv, true);
+  a.B = c.B;
+  a.H = c.H;
+  a.Hkv = c.H_kv;
+  a.G = group(c);
+  a.N = c.N;
+  a.Nk = c.N_k;
+  a.R = (int)dense_rows(c);
+  a.left = window(c.left, c);
+  a.right = window(c.right, c);
+  a.magic = ((uint64_t)1 << 40) / (uint64_t)a.G + 1;
+  a.scale = eff_scale(c);
+  a.sl2 = a.scale * LOG2E;
+  return a;
+}
+
+namespace {
+template <typename T, int D> hipError_t forward_t(const DenseArgs &a, hipStream_t st) {
+  dense_fwd_kernel<T, D><<<dim3((unsigned)(a.B * a.Hkv) * a.tiles * a.splits), 256, 0, st>>>(a);
+  hipError_t e = launched("dense_fwd_kernel", st);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.R, per = 256 / (D / 4);
+  dense_join_kernel<T, D><<<dim3((unsigned)((rows + per - 1) / per)), 256, 0, st>>>(a);
+  return launched("dense_join_kernel", st);
+}
+}  // namespace
+
+hipError_t launch_dense_forward(const mita_dense_cfg_t &c, const void *q, const void *k, const void *v,
+                                const int32_t *q_len, const int32_t *k_len, void *o, float *lse, void *ws,
+                                hipStream_t st) {
+  DenseArgs a = dense_args(c);
+  const DensePlan p = dense_plan(c);
+  const DenseFwdLayout L = dense_forward_layout(c);
+  a.q.p = (const char *)q;
+  a.k.p = (const char *)k;
+  a.v.p = (const char *)v;
+  a.o.p = (const char *)o;
+  a.q_len = q_len;
+  a.k_len = k_len;
+  a.lse = lse;
+  a.tiles = p.tiles;
+  a.splits = p.splits;
+  if (p.splits > 1) {
+    a.part_o = (float *)((char *)ws + L.part_o);
+    a.part_lse = (float *)((char *)ws + L.part_lse);
+  }
+  if (c.dtype == MITA_F32) return c.d == 64 ? forward_t<float, 64>(a, st) : forward_t<float, 128>(a, st);
+  return c.d == 64 ? forward_t<bf16_t, 64>(a, st) : forward_t<bf16_t, 128>(a, st);
+}
+
+}  // namespace mita

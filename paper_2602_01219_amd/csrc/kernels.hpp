@@ -204,4 +204,19 @@ struct TomeBufs {
 hipError_t launch_tome(const mita_cfg_t &c, const void *q, void *q_lm, int32_t *assign, const TomeBufs &b,
                        hipStream_t st);
 
+// Dense attention and its gradients (mita_dense_forward, mita_dense_backward).
+hipError_t launch_dense_forward(const mita_dense_cfg_t &c, const void *q, const void *k, const void *v,
+                                const int32_t *q_len, const int32_t *k_len, void *o, float *lse, void *ws,
+                                hipStream_t st);
+hipError_t launch_dense_backward(const mita_dense_cfg_t &c, const void *q, const void *k, const void *v, const void *o,
+                                 const float *lse, const void *dO, const int32_t *q_len, const int32_t *k_len, void *dq,
+                                 void *dk, void *dv, void *ws, hipStream_t st);
+
+// Layer norm of rows and its gradients (mita_norm_forward, mita_norm_backward).
+hipError_t launch_norm_forward(const mita_norm_cfg_t &c, const void *x, const void *w, const void *b, void *y,
+                               float *mean, float *rstd, hipStream_t st);
+hipError_t launch_norm_backward(const mita_norm_cfg_t &c, const void *x, const void *w, const float *mean,
+                                const float *rstd, const void *dy, void *dx, void *dw, void *db, void *ws,
+                                hipStream_t st);
+
 }  // namespace mita

@@ -2,12 +2,14 @@
 // the launch sequence of the forward pass (Algorithm 1 order).
 #include <hip/hip_runtime.h>
 
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <vector>
 
 #include "check.hpp"
 #include "kernels.hpp"
+#include "layer_check.hpp"
 
 using namespace mita;
 
@@ -363,6 +365,70 @@ int scratch_address(void **out) {
 
 }  // namespace
 
+namespace {
+
+int validate(const mita_dense_cfg_t *c) {
+  std::string msg;
+  const int st = check_dense(c, &msg);
+  return st == MITA_OK ? st : set_err(st, msg);
+}
+int validate(const mita_norm_cfg_t *c) {
+  std::string msg;
+  const int st = check_norm(c, &msg);
+  return st == MITA_OK ? st : set_err(st, msg);
+}
+
+int need_bytes(size_t need, const void *ws, size_t ws_bytes) {
+  if (need == 0) return MITA_OK;
+  if (!ws || ws_bytes < need)
+    return set_err(MITA_ERR_WORKSPACE, "workspace needs " + std::to_string(need) + " bytes, got " +
+                                           std::to_string(ws ? ws_bytes : 0));
+  if (((uintptr_t)ws & (WS_ALIGN - 1)) != 0) return set_err(MITA_ERR_INVALID_ARG, "workspace is not 256-byte aligned");
+  return MITA_OK;
+}
+
+// A pointer to elements of `e` bytes.
+int need_elem_ptr(const void *p, size_t e, const char *name) {
+  if (!p) return set_err(MITA_ERR_INVALID_ARG, std::string(name) + " is NULL");
+  if ((uintptr_t)p % e != 0) return set_err(MITA_ERR_INVALID_ARG, std::string(name) + " is not aligned to its elements");
+  return MITA_OK;
+}
+
+struct Buffer {
+  const char *name;
+  const void *p;
+  Strided s;
+  size_t e;  // bytes per element
+};
+Strided whole(int64_t n) { return Strided{{1, 1, 1}, {n, n, n}, n}; }
+Buffer bytes_of(const char *name, const void *p, size_t n) { return Buffer{name, p, whole((int64_t)n), 1}; }
+bool overlap(const Buffer &a, const Buffer &b) {
+  if (a.e == b.e) return may_overlap(a.p, a.s, b.p, b.s, a.e);
+  return overlaps(a.p, a.p ? (size_t)span_of(a.s) * a.e : 0, b.p, b.p ? (size_t)span_of(b.s) * b.e : 0);
+}
+// No output may share memory with an input or another output.
+int apart(std::initializer_list<Buffer> out, std::initializer_list<Buffer> in) {
+  for (const Buffer *a = out.begin(); a != out.end(); ++a) {
+    for (const Buffer &b : in)
+      if (overlap(*a, b)) return set_err(MITA_ERR_INVALID_ARG, std::string(a->name) + " overlaps " + b.name);
+    for (const Buffer *b = out.begin(); b != a; ++b)
+      if (overlap(*a, *b)) return set_err(MITA_ERR_INVALID_ARG, std::string(a->name) + " overlaps " + b->name);
+  }
+  return MITA_OK;
+}
+
+// Nothing is thrown across the ABI (building a message may run out of memory).
+template <typename F> int guarded(F &&f) {
+  try {
+    g_err.clear();
+    return f();
+  } catch (...) {
+    return MITA_ERR_HIP;
+  }
+}
+
+}  // namespace
+
 extern "C" {
 
 int mita_forward_noalloc(const mita_cfg_t *cfg, const void *q, const void *k, const void *v, void *o,
@@ -607,6 +673,125 @@ int mita_attend(const mita_cfg_t *cfg, const void *q, const void *q_lm, const vo
   return hip_status(
       launch_attend(*cfg, q, q_lm, v_lm, k_x, v_x, nullptr, perm, offsets, tile_start, o, pair_o, pair_lse, st),
       "attend");
+}
+
+int mita_dense_check(const mita_dense_cfg_t *cfg) {
+  return guarded([&]() -> int {
+    return validate(cfg);
+  });
+}
+
+size_t mita_dense_workspace_size(const mita_dense_cfg_t *cfg, int which) { return dense_workspace_size(cfg, which); }
+
+int mita_dense_forward(const mita_dense_cfg_t *cfg, const void *q, const void *k, const void *v, const int32_t *q_len,
+                       const int32_t *k_len, void *o, float *lse, void *ws, size_t ws_bytes, mita_stream_t stream) {
+  return guarded([&]() -> int {
+    TRY(validate(cfg));
+    TRY(need_ptr(q, "q"));
+    TRY(need_ptr(k, "k"));
+    TRY(need_ptr(v, "v"));
+    TRY(need_ptr(o, "o"));
+    if (q_len) TRY(need_elem_ptr(q_len, 4, "q_len"));
+    if (k_len) TRY(need_elem_ptr(k_len, 4, "k_len"));
+    if (lse) TRY(need_elem_ptr(lse, 4, "lse"));
+    const size_t need = dense_workspace_size(cfg, MITA_WS_FORWARD), e = elem_bytes(*cfg);
+    TRY(need_bytes(need, ws, ws_bytes));
+    const Buffer bq{"q", q, strided_q(*cfg, cfg->q), e}, bk{"k", k, strided_k(*cfg, cfg->k), e};
+    const Buffer bv{"v", v, strided_k(*cfg, cfg->v), e}, bo{"o", o, strided_q(*cfg, cfg->o), e};
+    TRY(apart({bo, bytes_of("lse", lse, (size_t)cfg->B * cfg->H * cfg->N * 4), bytes_of("ws", need ? ws : nullptr, need)},
+              {bq, bk, bv, bytes_of("q_len", q_len, (size_t)cfg->B * 4), bytes_of("k_len", k_len, (size_t)cfg->B * 4)}));
+    return hip_status(launch_dense_forward(*cfg, q, k, v, q_len, k_len, o, lse, ws, (hipStream_t)stream), "dense forward");
+  });
+}
+
+int mita_dense_backward(const mita_dense_cfg_t *cfg, const void *q, const void *k, const void *v, const void *o,
+                        const float *lse, const void *dO, const int32_t *q_len, const int32_t *k_len, void *dq, void *dk,
+                        void *dv, void *ws, size_t ws_bytes, mita_stream_t stream) {
+  return guarded([&]() -> int {
+    TRY(validate(cfg));
+    TRY(need_ptr(q, "q"));
+    TRY(need_ptr(k, "k"));
+    TRY(need_ptr(v, "v"));
+    TRY(need_ptr(o, "o"));
+    TRY(need_elem_ptr(lse, 4, "lse"));
+    TRY(need_ptr(dO, "dO"));
+    TRY(need_ptr(dq, "dq"));
+    TRY(need_ptr(dk, "dk"));
+    TRY(need_ptr(dv, "dv"));
+    if (q_len) TRY(need_elem_ptr(q_len, 4, "q_len"));
+    if (k_len) TRY(need_elem_ptr(k_len, 4, "k_len"));
+    const size_t need = dense_workspace_size(cfg, MITA_WS_BACKWARD), e = elem_bytes(*cfg);
+    TRY(need_bytes(need, ws, ws_bytes));
+    const Buffer bq{"q", q, strided_q(*cfg, cfg->q), e}, bk{"k", k, strided_k(*cfg, cfg->k), e};
+    const Buffer bv{"v", v, strided_k(*cfg, cfg->v), e}, bo{"o", o, strided_q(*cfg, cfg->o), e};
+    const Buffer bdO{"dO", dO, strided_q(*cfg, cfg->dO), e}, bdq{"dq", dq, strided_q(*cfg, cfg->dq), e};
+    const Buffer bdk{"dk", dk, strided_k(*cfg, cfg->dk), e}, bdv{"dv", dv, strided_k(*cfg, cfg->dv), e};
+    TRY(apart({bdq, bdk, bdv, bytes_of("ws", ws, need)},
+              {bq, bk, bv, bo, bdO, bytes_of("lse", lse, (size_t)cfg->B * cfg->H * cfg->N * 4),
+               bytes_of("q_len", q_len, (size_t)cfg->B * 4), bytes_of("k_len", k_len, (size_t)cfg->B * 4)}));
+    return hip_status(
+        launch_dense_backward(*cfg, q, k, v, o, lse, dO, q_len, k_len, dq, dk, dv, ws, (hipStream_t)stream),
+        "dense backward");
+  });
+}
+
+int mita_norm_check(const mita_norm_cfg_t *cfg) {
+  return guarded([&]() -> int {
+    return validate(cfg);
+  });
+}
+
+size_t mita_norm_workspace_size(const mita_norm_cfg_t *cfg) { return norm_workspace_size(cfg); }
+
+int mita_norm_forward(const mita_norm_cfg_t *cfg, const void *x, const void *w, const void *b, void *y, float *mean,
+                      float *rstd, mita_stream_t stream) {
+  return guarded([&]() -> int {
+    TRY(validate(cfg));
+    const size_t e = elem_bytes(*cfg), ew = cfg->wdtype == MITA_F32 ? 4 : 2, rows = (size_t)norm_rows(*cfg);
+    TRY(need_elem_ptr(x, e, "x"));
+    TRY(need_elem_ptr(y, e, "y"));
+    if (w) TRY(need_elem_ptr(w, ew, "w"));
+    if (b) TRY(need_elem_ptr(b, ew, "b"));
+    if (mean) TRY(need_elem_ptr(mean, 4, "mean"));
+    if (rstd) TRY(need_elem_ptr(rstd, 4, "rstd"));
+    const Strided sx = strided_rows(*cfg, cfg->x), sy = strided_rows(*cfg, cfg->y);
+    const Buffer bx{"x", x, sx, e}, by{"y", y, sy, e};
+    const Buffer bw = bytes_of("w", w, cfg->C * ew), bb = bytes_of("b", b, cfg->C * ew);
+    const Buffer bm = bytes_of("mean", mean, rows * 4), br = bytes_of("rstd", rstd, rows * 4);
+    if (!same_rows(x, sx, y, sy)) TRY(apart({by}, {bx}));
+    TRY(apart({by, bm, br}, {bw, bb}));
+    TRY(apart({bm, br}, {bx}));
+    return hip_status(launch_norm_forward(*cfg, x, w, b, y, mean, rstd, (hipStream_t)stream), "norm forward");
+  });
+}
+
+int mita_norm_backward(const mita_norm_cfg_t *cfg, const void *x, const void *w, const float *mean, const float *rstd,
+                       const void *dy, void *dx, void *dw, void *db, void *ws, size_t ws_bytes, mita_stream_t stream) {
+  return guarded([&]() -> int {
+    TRY(validate(cfg));
+    const size_t e = elem_bytes(*cfg), ew = cfg->wdtype == MITA_F32 ? 4 : 2, rows = (size_t)norm_rows(*cfg);
+    TRY(need_elem_ptr(x, e, "x"));
+    TRY(need_elem_ptr(dy, e, "dy"));
+    TRY(need_elem_ptr(mean, 4, "mean"));
+    TRY(need_elem_ptr(rstd, 4, "rstd"));
+    if (w) TRY(need_elem_ptr(w, ew, "w"));
+    if (dx) TRY(need_elem_ptr(dx, e, "dx"));
+    if (dw) TRY(need_elem_ptr(dw, ew, "dw"));
+    if (db) TRY(need_elem_ptr(db, ew, "db"));
+    if (!dx && !dw && !db) return set_err(MITA_ERR_INVALID_ARG, "dx, dw and db are all NULL");
+    const size_t need = dw || db ? norm_workspace_size(cfg) : 0;
+    TRY(need_bytes(need, ws, ws_bytes));
+    const Strided sx = strided_rows(*cfg, cfg->x), sdy = strided_rows(*cfg, cfg->dy), sdx = strided_rows(*cfg, cfg->dx);
+    const Buffer bx{"x", x, sx, e}, bdy{"dy", dy, sdy, e}, bdx{"dx", dx, sdx, e};
+    const Buffer bw = bytes_of("w", w, cfg->C * ew), bm = bytes_of("mean", mean, rows * 4);
+    const Buffer br = bytes_of("rstd", rstd, rows * 4), bdw = bytes_of("dw", dw, cfg->C * ew);
+    const Buffer bdb = bytes_of("db", db, cfg->C * ew), bws = bytes_of("ws", need ? ws : nullptr, need);
+    if (!same_rows(dy, sdy, dx, sdx)) TRY(apart({bdx}, {bdy}));
+    TRY(apart({bdx, bdw, bdb, bws}, {bx, bw, bm, br}));
+    TRY(apart({bdw, bdb, bws}, {bdy}));
+    return hip_status(launch_norm_backward(*cfg, x, w, mean, rstd, dy, dx, dw, db, ws, (hipStream_t)stream),
+                      "norm backward");
+  });
 }
 
 int mita_timer_create(mita_timer_t **timer, int max_calls) {

@@ -37,13 +37,32 @@ EXPORTED = ("mita_check", "mita_workspace_size", "mita_status_string", "mita_las
             "mita_timer_create", "mita_timer_destroy", "mita_timer_reset", "mita_timer_read",
             "mita_forward_timed", "mita_forward_fallbacks", "mita_select_plan", "mita_timer_launches",
             "mita_forward_noalloc", "mita_landmarks_select", "mita_forward_lm", "mita_forward_lm_timed",
-            "mita_backward", "mita_backward_timed", "mita_landmarks_tome")
+            "mita_backward", "mita_backward_timed", "mita_landmarks_tome",
+            "mita_dense_check", "mita_dense_workspace_size", "mita_dense_forward", "mita_dense_backward",
+            "mita_norm_check", "mita_norm_workspace_size", "mita_norm_forward", "mita_norm_backward")
 
 
 class CfgStruct(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("B", "H", "N", "d", "grid_h", "grid_w", "M", "lm_h", "lm_w", "k", "s", "use_shared",
                  "use_routed", "dtype")] + [("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class StridesStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("b", "h", "n")]
+
+
+class DenseCfgStruct(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "H", "H_kv", "N", "N_k", "d", "dtype", "left", "right")]
+                + [("scale", ctypes.c_float)]
+                + [(n, StridesStruct) for n in ("q", "k", "v", "o", "dO", "dq", "dk", "dv")])
+
+
+class NormCfgStruct(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32 * 3), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("wdtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("x", ctypes.c_int64 * 3), ("y", ctypes.c_int64 * 3), ("dy", ctypes.c_int64 * 3),
+                ("dx", ctypes.c_int64 * 3)]
 
 
 class MitaError(RuntimeError):
@@ -65,6 +84,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib = ctypes.CDLL(path)
     P, I, Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
     cfgp = ctypes.POINTER(CfgStruct)
+    densep, normp = ctypes.POINTER(DenseCfgStruct), ctypes.POINTER(NormCfgStruct)
     sig = {
         "mita_check": (I, [cfgp]),
         "mita_workspace_size": (Z, [cfgp, I]),
@@ -83,6 +103,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "mita_landmarks_tome": (I, [cfgp, P, P, P, P, Z, P]),
         "mita_backward_timed": (I, [cfgp, P, P, P, P, P, P, P, P, P, Z, P, P]),
         "mita_scores": (I, [cfgp, P, P, P, P, P, P, Z, P]),
+        "mita_dense_check": (I, [densep]),
+        "mita_dense_workspace_size": (Z, [densep, I]),
+        "mita_dense_forward": (I, [densep, P, P, P, P, P, P, P, P, Z, P]),
+        "mita_dense_backward": (I, [densep, P, P, P, P, P, P, P, P, P, P, P, P, Z, P]),
+        "mita_norm_check": (I, [normp]),
+        "mita_norm_workspace_size": (Z, [normp]),
+        "mita_norm_forward": (I, [normp, P, P, P, P, P, P, P]),
+        "mita_norm_backward": (I, [normp, P, P, P, P, P, P, P, P, P, Z, P]),
         "mita_topk": (I, [cfgp, P, P, P, Z, P]),
         "mita_gather": (I, [cfgp, P, P, P, P, P, P]),
         "mita_route": (I, [cfgp, P, P, P, P, P, P, Z, P]),
@@ -354,6 +382,281 @@ def attend(cfg: Config, q, q_lm, v_lm, k_x, v_x, perm, offsets, o=None, ws=None,
     _check(lib.mita_attend(ctypes.byref(cfg.struct()), _p(q), _p(q_lm), _p(v_lm), _p(k_x), _p(v_x), _p(perm),
                            _p(offsets), _p(o), _p(ws), nws, _stream(stream)))
     return o
+
+
+# ---------------------------------------------------------------------------
+# Dense attention and layer norm
+# ---------------------------------------------------------------------------
+@dataclass(frozen=True)
+class DenseConfig:
+    """Dense attention problem (mita_dense_cfg_t without the strides, which are
+    the tensors' own). H_kv = 0 means H, N_k = 0 means N; a query at position p
+    sees the keys p - left .. p + right (-1: no bound; right = 0: causal)."""
+    B: int
+    H: int
+    N: int
+    d: int
+    H_kv: int = 0
+    N_k: int = 0
+    dtype: str = "bf16"          # "f32" | "bf16"
+    left: int = -1
+    right: int = -1
+    scale: float = 0.0           # 0 -> 1/sqrt(d)
+
+    @property
+    def q_shape(self):
+        return (self.B, self.H, self.N, self.d)
+
+    @property
+    def k_shape(self):
+        return (self.B, self.H_kv or self.H, self.N_k or self.N, self.d)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == "f32" else torch.bfloat16
+
+    def struct(self, **tensors) -> DenseCfgStruct:
+        c = DenseCfgStruct(self.B, self.H, self.H_kv or self.H, self.N, self.N_k or self.N, self.d,
+                           _dtype_code(self.dtype), self.left, self.right, float(self.scale))
+        for name, t in tensors.items():
+            setattr(c, name, StridesStruct(*_strides(t)))
+        return c
+
+
+@dataclass(frozen=True)
+class NormConfig:
+    """Layer norm of rows of C elements (mita_norm_cfg_t without the strides):
+    rows is the shape in front of the last dimension, up to three dimensions."""
+    rows: tuple
+    C: int
+    dtype: str = "bf16"          # x, y and their gradients
+    wdtype: str = "f32"          # weight, bias and their gradients
+    eps: float = 1e-5
+
+    @property
+    def shape(self):
+        return tuple(self.rows) + (self.C,)
+
+    def struct(self, **tensors) -> NormCfgStruct:
+        if not 1 <= len(self.rows) <= 3:
+            raise ValueError("rows must have one to three dimensions")
+        pad = 3 - len(self.rows)
+        c = NormCfgStruct()
+        c.n = (ctypes.c_int32 * 3)(*([1] * pad + [int(n) for n in self.rows]))
+        c.C, c.dtype, c.wdtype, c.eps = self.C, _dtype_code(self.dtype), _dtype_code(self.wdtype), float(self.eps)
+        for name, t in tensors.items():
+            s = [0] * pad + _row_strides(t)
+            if any(s):
+                # dimensions in front of the rows have one entry: any distance will do
+                setattr(c, name, (ctypes.c_int64 * 3)(*[x or self.C for x in s[:pad]], *s[pad:]))
+        return c
+
+
+def _dtype_code(name: str) -> int:
+    if name not in ("f32", "bf16"):
+        raise ValueError(f"dtype must be 'f32' or 'bf16', got {name!r}")
+    return MITA_F32 if name == "f32" else MITA_BF16
+
+
+def _row_strides(t):
+    """Distances of a tensor's leading dimensions (a dimension of one entry: that
+    of a contiguous tensor)."""
+    out, inner = [], t.shape[-1]
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        out.append(inner if n == 1 else s)
+        inner *= n
+    out.reverse()
+    if not any(out):
+        raise ValueError("a tensor that repeats one row everywhere has to be made contiguous")
+    return out
+
+
+def _strides(t):
+    s = _row_strides(t)
+    if t.shape[2] > 1 and s[2] == 0:
+        raise ValueError("tokens must not be repeated (stride 0 between tokens)")
+    return s
+
+
+def _tensor(t, name, shape, dtype, device):
+    """A device tensor of this shape and type whose last dimension is dense."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a tensor on the GPU")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t
+
+
+def _packed(t, name, shape, dtype, device):
+    """The same, contiguous."""
+    if not _tensor(t, name, shape, dtype, device).is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _lengths(t, name, B, device):
+    return None if t is None else _packed(t, name, (B,), torch.int32, device)
+
+
+def _workspace(ws, need, device):
+    if ws is None:
+        return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
+    if not ws.is_cuda or ws.device != device or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on the tensors' device")
+    return ws, ws.numel() * ws.element_size()
+
+
+def _stream_on(stream, device):
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    if s.device != device:
+        raise ValueError(f"the stream is on {s.device}, the tensors on {device}")
+    return ctypes.c_void_p(s.cuda_stream)
+
+
+def dense_check(cfg: DenseConfig) -> int:
+    return load_library().mita_dense_check(ctypes.byref(cfg.struct()))
+
+
+def dense_workspace_size(cfg: DenseConfig, which: int = WS_FORWARD) -> int:
+    return int(load_library().mita_dense_workspace_size(ctypes.byref(cfg.struct()), which))
+
+
+def dense_forward(cfg: DenseConfig, q, k, v, q_len=None, k_len=None, o=None, lse=None, want_lse=True, ws=None,
+                  stream=None):
+    """Dense attention (mita_dense_forward): (o [B, H, N, d], lse [B, H, N] fp32
+    or None). q, k, v may be strided (their last dimension dense); q_len, k_len
+    are [B] int32 device tensors."""
+    lib = load_library()
+    _tensor(q, "q", cfg.q_shape, cfg.torch_dtype, None)
+    dev = q.device
+    _tensor(k, "k", cfg.k_shape, cfg.torch_dtype, dev)
+    _tensor(v, "v", cfg.k_shape, cfg.torch_dtype, dev)
+    _lengths(q_len, "q_len", cfg.B, dev)
+    _lengths(k_len, "k_len", cfg.B, dev)
+    with torch.cuda.device(dev):
+        o = _out_like(q) if o is None else _tensor(o, "o", cfg.q_shape, cfg.torch_dtype, dev)
+        if lse is None:
+            lse = torch.empty(cfg.q_shape[:3], dtype=torch.float32, device=dev) if want_lse else None
+        else:
+            _packed(lse, "lse", cfg.q_shape[:3], torch.float32, dev)
+        c = cfg.struct(q=q, k=k, v=v, o=o)
+        ws, nws = _workspace(ws, int(lib.mita_dense_workspace_size(ctypes.byref(c), WS_FORWARD)), dev)
+        _check(lib.mita_dense_forward(ctypes.byref(c), _p(q), _p(k), _p(v), _p(q_len), _p(k_len), _p(o), _p(lse),
+                                      _p(ws), nws, _stream_on(stream, dev)))
+    return o, lse
+
+
+def dense_backward(cfg: DenseConfig, q, k, v, o, lse, dO, q_len=None, k_len=None, dq=None, dk=None, dv=None, ws=None,
+                   stream=None):
+    """Gradients (dq, dk, dv) of dense_forward's o for the upstream gradient dO
+    (mita_dense_backward)."""
+    lib = load_library()
+    _tensor(q, "q", cfg.q_shape, cfg.torch_dtype, None)
+    dev, dt = q.device, cfg.torch_dtype
+    for t, name, shape in ((k, "k", cfg.k_shape), (v, "v", cfg.k_shape), (o, "o", cfg.q_shape),
+                           (dO, "dO", cfg.q_shape)):
+        _tensor(t, name, shape, dt, dev)
+    _packed(lse, "lse", cfg.q_shape[:3], torch.float32, dev)
+    _lengths(q_len, "q_len", cfg.B, dev)
+    _lengths(k_len, "k_len", cfg.B, dev)
+    with torch.cuda.device(dev):
+        dq = _out_like(q) if dq is None else _tensor(dq, "dq", cfg.q_shape, dt, dev)
+        dk = _out_like(k) if dk is None else _tensor(dk, "dk", cfg.k_shape, dt, dev)
+        dv = _out_like(v) if dv is None else _tensor(dv, "dv", cfg.k_shape, dt, dev)
+        c = cfg.struct(q=q, k=k, v=v, o=o, dO=dO, dq=dq, dk=dk, dv=dv)
+        ws, nws = _workspace(ws, int(lib.mita_dense_workspace_size(ctypes.byref(c), WS_BACKWARD)), dev)
+        _check(lib.mita_dense_backward(ctypes.byref(c), _p(q), _p(k), _p(v), _p(o), _p(lse), _p(dO), _p(q_len),
+                                       _p(k_len), _p(dq), _p(dk), _p(dv), _p(ws), nws, _stream_on(stream, dev)))
+    return dq, dk, dv
+
+
+def _out_like(t):
+    """A tensor for an output beside t: tokens before heads in memory where t has
+    them so (a projection's layout), else contiguous."""
+    if t.dim() == 4 and t.shape[1] > 1 and t.shape[2] > 1 and t.stride(1) < t.stride(2):
+        B, H, N, d = t.shape
+        return torch.empty((B, N, H, d), dtype=t.dtype, device=t.device).transpose(1, 2)
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def norm_check(cfg: NormConfig) -> int:
+    return load_library().mita_norm_check(ctypes.byref(cfg.struct()))
+
+
+def norm_workspace_size(cfg: NormConfig) -> int:
+    """Bytes of workspace norm_backward needs for the weight's gradients."""
+    return int(load_library().mita_norm_workspace_size(ctypes.byref(cfg.struct())))
+
+
+def _norm_types(cfg):
+    return (torch.float32 if cfg.dtype == "f32" else torch.bfloat16,
+            torch.float32 if cfg.wdtype == "f32" else torch.bfloat16)
+
+
+def norm_forward(cfg: NormConfig, x, w=None, b=None, y=None, mean=None, rstd=None, want_stats=True, stream=None):
+    """Layer norm (mita_norm_forward): (y like x, mean and rstd [rows] fp32 or
+    None). x may be strided (its last dimension dense)."""
+    lib = load_library()
+    dt, wt = _norm_types(cfg)
+    _tensor(x, "x", cfg.shape, dt, None)
+    dev = x.device
+    for t, name in ((w, "w"), (b, "b")):
+        if t is not None:
+            _packed(t, name, (cfg.C,), wt, dev)
+    with torch.cuda.device(dev):
+        y = _out_like(x) if y is None else _tensor(y, "y", cfg.shape, dt, dev)
+        stats = []
+        for t, name in ((mean, "mean"), (rstd, "rstd")):
+            if t is None:
+                t = torch.empty(tuple(cfg.rows), dtype=torch.float32, device=dev) if want_stats else None
+            else:
+                _packed(t, name, cfg.rows, torch.float32, dev)
+            stats.append(t)
+        mean, rstd = stats
+        c = cfg.struct(x=x, y=y)
+        _check(lib.mita_norm_forward(ctypes.byref(c), _p(x), _p(w), _p(b), _p(y), _p(mean), _p(rstd),
+                                     _stream_on(stream, dev)))
+    return y, mean, rstd
+
+
+def norm_backward(cfg: NormConfig, x, mean, rstd, dy, w=None, dx=None, dw=None, db=None, want_dx=True,
+                  want_weights=True, ws=None, stream=None):
+    """Gradients (dx, dw, db) of norm_forward (mita_norm_backward); dx, or dw and
+    db, are None unless wanted."""
+    lib = load_library()
+    dt, wt = _norm_types(cfg)
+    _tensor(x, "x", cfg.shape, dt, None)
+    dev = x.device
+    _tensor(dy, "dy", cfg.shape, dt, dev)
+    _packed(mean, "mean", cfg.rows, torch.float32, dev)
+    _packed(rstd, "rstd", cfg.rows, torch.float32, dev)
+    if w is not None:
+        _packed(w, "w", (cfg.C,), wt, dev)
+    with torch.cuda.device(dev):
+        if dx is not None:
+            _tensor(dx, "dx", cfg.shape, dt, dev)
+        elif want_dx:
+            dx = _out_like(x)
+        grads = []
+        for t, name in ((dw, "dw"), (db, "db")):
+            if t is None:
+                t = torch.empty(cfg.C, dtype=wt, device=dev) if want_weights else None
+            else:
+                _packed(t, name, (cfg.C,), wt, dev)
+            grads.append(t)
+        dw, db = grads
+        c = cfg.struct(x=x, dy=dy, **({"dx": dx} if dx is not None else {}))
+        need = int(lib.mita_norm_workspace_size(ctypes.byref(c))) if dw is not None or db is not None else 0
+        ws, nws = _workspace(ws, need, dev)
+        _check(lib.mita_norm_backward(ctypes.byref(c), _p(x), _p(w), _p(mean), _p(rstd), _p(dy), _p(dx), _p(dw), _p(db),
+                                      _p(ws), nws, _stream_on(stream, dev)))
+    return dx, dw, db
 
 
 class Timer:

@@ -1,0 +1,164 @@
+// Host test of layer_check.hpp: validation, overlap of strided tensors, launch
+// plans and workspace layouts of the dense attention and the layer norm.
+#include <cstdio>
+#include <cstdlib>
+#include <set>
+#include <vector>
+
+#include "../../paper_2602_01219_amd/csrc/layer_check.hpp"
+
+using namespace mita;
+
+#define CHECK(x)                                             \
+  do {                                                       \
+    if (!(x)) {                                              \
+      printf("failed: %s (line %d)\n", #x, __LINE__);        \
+      return 1;                                              \
+    }                                                        \
+  } while (0)
+
+static mita_dense_cfg_t dense(int B, int H, int Hk, int N, int Nk, int d, int dtype) {
+  mita_dense_cfg_t c{};
+  c.B = B, c.H = H, c.H_kv = Hk, c.N = N, c.N_k = Nk, c.d = d, c.dtype = dtype;
+  c.left = c.right = -1;
+  return c;
+}
+
+static void elements(std::multiset<int64_t> &out, const Strided &t, int64_t base) {
+  for (int64_t i = 0; i < t.n[0]; ++i)
+    for (int64_t j = 0; j < t.n[1]; ++j)
+      for (int64_t k = 0; k < t.n[2]; ++k)
+        for (int64_t l = 0; l < t.len; ++l) out.insert(base + i * t.s[0] + j * t.s[1] + k * t.s[2] + l);
+}
+
+int main() {
+  mita_dense_cfg_t c = dense(2, 8, 2, 100, 300, 64, MITA_BF16);
+  CHECK(check_dense(&c, nullptr) == MITA_OK);
+  CHECK(check_dense(nullptr, nullptr) == MITA_ERR_INVALID_ARG);
+  struct Bad {
+    void (*f)(mita_dense_cfg_t &);
+    int status;
+  };
+  const Bad bad[] = {
+      {[](mita_dense_cfg_t &x) { x.H_kv = 3; }, MITA_ERR_INVALID_ARG},
+      {[](mita_dense_cfg_t &x) { x.N_k = 0; }, MITA_ERR_INVALID_ARG},
+      {[](mita_dense_cfg_t &x) { x.d = 96; }, MITA_ERR_UNSUPPORTED},
+      {[](mita_dense_cfg_t &x) { x.dtype = 2; }, MITA_ERR_UNSUPPORTED},
+      {[](mita_dense_cfg_t &x) { x.N = MITA_DENSE_MAX_N + 1; }, MITA_ERR_UNSUPPORTED},
+      {[](mita_dense_cfg_t &x) { x.left = -2; }, MITA_ERR_INVALID_ARG},
+      {[](mita_dense_cfg_t &x) { x.scale = -1.f; }, MITA_ERR_INVALID_ARG},
+      {[](mita_dense_cfg_t &x) { x.scale = NAN; }, MITA_ERR_INVALID_ARG},
+      {[](mita_dense_cfg_t &x) { x.q = {51200, 6400, 63}; }, MITA_ERR_INVALID_ARG},   // tokens overlap
+      {[](mita_dense_cfg_t &x) { x.q = {51200, 6400, 68}; }, MITA_ERR_INVALID_ARG},   // not 16 bytes
+      {[](mita_dense_cfg_t &x) { x.k = {51200, -64, 128}; }, MITA_ERR_INVALID_ARG},
+      {[](mita_dense_cfg_t &x) { x.k = {1, 0, 0}; }, MITA_ERR_INVALID_ARG},           // one token for all
+      {[](mita_dense_cfg_t &x) { x.o = {51200, 0, 64}; }, MITA_ERR_INVALID_ARG},      // heads written to one place
+      {[](mita_dense_cfg_t &x) { x.dv = {64, 19200, 64}; }, MITA_ERR_INVALID_ARG},
+      {[](mita_dense_cfg_t &x) { x.v = {51200, 64, (int64_t)MITA_DENSE_MAX_STRIDE + 8}; }, MITA_ERR_INVALID_ARG},
+      {[](mita_dense_cfg_t &x) { x.H = 8192; x.H_kv = 8192; }, MITA_ERR_UNSUPPORTED},
+      {[](mita_dense_cfg_t &x) { x.H = 4096; x.H_kv = 1; x.N = 65536; }, MITA_ERR_UNSUPPORTED},
+  };
+  for (const Bad &b : bad) {
+    mita_dense_cfg_t x = c;
+    b.f(x);
+    CHECK(check_dense(&x, nullptr) == b.status);
+    CHECK(dense_workspace_size(&x, MITA_WS_FORWARD) == 0 && dense_workspace_size(&x, MITA_WS_BACKWARD) == 0);
+  }
+  // projections' layouts and repeated inputs
+  c.q = {100 * 512, 64, 512};
+  c.k = {300 * 128, 0, 64};
+  CHECK(check_dense(&c, nullptr) == MITA_OK);
+  c.d = 128, c.q = c.k = {0, 0, 0};
+  CHECK(check_dense(&c, nullptr) == MITA_OK);
+
+  // overlap of interleaved tensors: against the element sets
+  srand(1);
+  int seen[2] = {0, 0};
+  for (int it = 0; it < 20000; ++it) {
+    Strided a{}, b{};
+    a.len = 1 + rand() % 4;
+    int64_t ext = a.len;
+    int order[3] = {0, 1, 2};
+    std::swap(order[rand() % 3], order[rand() % 3]);
+    int64_t n[3];
+    for (int i = 0; i < 3; ++i) n[i] = 1 + rand() % 3;
+    for (int i : order) {
+      a.s[i] = ext + rand() % 5;
+      ext += (n[i] - 1) * a.s[i];
+    }
+    b = a;
+    for (int i = 0; i < 3; ++i) {
+      a.n[i] = 1 + rand() % n[i];
+      b.n[i] = 1 + rand() % n[i];
+    }
+    const int64_t delta = rand() % (2 * ext) - ext;
+    std::multiset<int64_t> ea, eb;
+    elements(ea, a, 1000);
+    elements(eb, b, 1000 + delta);
+    bool hit = false;
+    for (int64_t x : eb) hit |= ea.count(x) > 0;
+    CHECK(nested(a) && nested(b));
+    const bool said = may_overlap((void *)(uintptr_t)(4000), a, (void *)(uintptr_t)(4000 + 4 * delta), b, 4);
+    if (hit) CHECK(said);  // never missed
+    // and told apart where the two differ only in their first element
+    bool alike = true;
+    for (int i = 0; i < 3; ++i) alike &= a.n[i] == b.n[i];
+    if (alike) CHECK(said == hit);
+    ++seen[hit];
+  }
+  CHECK(seen[0] > 1000 && seen[1] > 1000);
+
+  // plans: splits only where workgroups are few, never without keys, workspaces to match
+  for (int B : {1, 3, 64})
+    for (int H : {1, 6, 32})
+      for (int N : {1, 17, 500, 5000})
+        for (int Nk : {1, 130, 4096, 100000})
+          for (int w : {-1, 0, 700}) {
+            mita_dense_cfg_t x = dense(B, H, 1, N, Nk, 64, MITA_BF16);
+            x.left = w;
+            x.right = w < 0 ? -1 : 0;
+            const DensePlan p = dense_plan(x);
+            const DenseBwdPlan q = dense_bwd_plan(x);
+            CHECK(p.tiles >= 1 && (int64_t)p.tiles * DENSE_TQ >= dense_rows(x));
+            CHECK(p.splits >= 1 && p.splits <= DENSE_MAX_SPLITS);
+            CHECK(q.qsplits >= 1 && q.ksplits >= 1 && q.ktiles * DENSE_KB >= Nk);
+            if (p.splits > 1) CHECK(slices(x) * p.tiles < 2 * CUS);
+            const size_t rows = (size_t)slices(x) * dense_rows(x);
+            CHECK(dense_workspace_size(&x, MITA_WS_FORWARD) >= (p.splits > 1 ? rows * p.splits * 65 * 4 : 0));
+            const DenseBwdLayout L = dense_backward_layout(x);
+            CHECK(L.D - L.lse >= ((size_t)slices(x) * q.qtiles * DENSE_TQ + 64) * 4);
+            CHECK(L.total >= L.part_v + (q.ksplits > 1 ? (size_t)slices(x) * Nk * q.ksplits * 64 * 4 : 0));
+          }
+
+  // layer norm
+  mita_norm_cfg_t m{};
+  m.n[0] = 1, m.n[1] = 1, m.n[2] = 100, m.C = 768, m.dtype = MITA_BF16, m.wdtype = MITA_F32, m.eps = 1e-5f;
+  CHECK(check_norm(&m, nullptr) == MITA_OK);
+  for (int C = 1; C <= MITA_NORM_MAX_C; C = C < 20000 ? C + 1 : C * 2)
+    for (int t : {MITA_F32, MITA_BF16})
+      for (bool vec : {false, true}) {
+        mita_norm_cfg_t x = m;
+        x.C = C, x.dtype = t;
+        if (vec && C % (16 / (int)elem_bytes(x))) continue;
+        const NormPlan p = norm_plan(x, vec);
+        if (p.p) CHECK((int64_t)p.ve * p.tpr * p.p >= C);
+        CHECK(norm_workspace_size(&x) >= (size_t)norm_bwd_blocks(x, p) * 2 * C * 4);
+      }
+  {
+    mita_norm_cfg_t x = m;
+    x.C = 0;
+    CHECK(check_norm(&x, nullptr) == MITA_ERR_INVALID_ARG);
+    x = m, x.C = MITA_NORM_MAX_C + 1;
+    CHECK(check_norm(&x, nullptr) == MITA_ERR_UNSUPPORTED && norm_workspace_size(&x) == 0);
+    x = m, x.eps = 0.f;
+    CHECK(check_norm(&x, nullptr) == MITA_ERR_INVALID_ARG);
+    x = m, x.n[0] = x.n[1] = x.n[2] = 65536;
+    CHECK(check_norm(&x, nullptr) == MITA_ERR_UNSUPPORTED);
+    x = m, x.wdtype = 7;
+    CHECK(check_norm(&x, nullptr) == MITA_ERR_UNSUPPORTED);
+    x = m, x.n[1] = 4, x.y[0] = 768, x.y[1] = 0, x.y[2] = 768;
+    CHECK(check_norm(&x, nullptr) == MITA_ERR_INVALID_ARG);
+  }
+  printf("layer checks ok\n");
+  return 0;
+}
