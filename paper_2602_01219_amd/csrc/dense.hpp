@@ -56,12 +56,32 @@ __device__ __forceinline__ void copy4(const void *src, char *dst) {
   __builtin_amdgcn_global_load_lds(src, (lds_void_t *)dst, 4, 0, 0);
 }
 
+// The same copy without the waits that the compiler sets before LDS reads that it
+// cannot tell apart from it (it waits for every copy in flight where control flow
+// meets): the caller waits with wait_copies. dst is the same for the whole wave.
+__device__ __forceinline__ void copy16_unwaited(const void *src, char *dst) {
+  const uint32_t at = (uint32_t)(uintptr_t)(lds_void_t *)dst;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(at) : "memory");
+}
+
 // The copies this wave issued have landed, and those of every wave once all are
 // here. (The barrier alone does not wait for them: a wave that reads none of the
 // tile, or reads it behind the barrier, would pass with its own in flight.)
 __device__ __forceinline__ void tile_barrier() {
   wait_loads();
   __syncthreads();
+}
+
+// All but this wave's last N copies have landed; all its LDS reads have returned.
+template <int N> __device__ __forceinline__ void wait_copies() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("" ::: "memory");
 }
 
 // A tile's copy into LDS by DMA (global_load_lds_dwordx4), NW waves: lane l of

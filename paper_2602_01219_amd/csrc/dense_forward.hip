@@ -25,12 +25,10 @@ template <int D> struct DenseState {
   }
 };
 
-// 32 keys of a staged tile (rows 32 kb ..): scores, online softmax, values. lo and
-// hi bound the column's visible keys, counted from the block's first.
-template <typename T, int D, bool MASKED>
-__device__ __forceinline__ void dense_step(DenseState<D> &st, const char *Kt, const char *Vt, const TileAddr<T, D> &ad,
-                                           int kb, const uint4 (&q)[RowTile<T, D>::NS], float sl2, int lo, int hi) {
-  f32x16 s = tile_rows<T, D>(Kt, ad, kb, q, splat16(0.f));
+// The online softmax of 32 scores: s becomes the weights. lo and hi bound the
+// column's visible keys, counted from the block's first.
+template <int D, bool MASKED>
+__device__ __forceinline__ void dense_weights(DenseState<D> &st, f32x16 &s, float sl2, int lo, int hi) {
   const int g = (threadIdx.x & 63) >> 5;
   if (MASKED) {
 #pragma unroll
@@ -60,7 +58,37 @@ __device__ __forceinline__ void dense_step(DenseState<D> &st, const char *Kt, co
     s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], sl2, st.nm));
     st.l += s[i];
   }
+}
+
+// 32 keys of a staged tile (rows 32 kb ..): scores, online softmax, values.
+template <typename T, int D, bool MASKED>
+__device__ __forceinline__ void dense_step(DenseState<D> &st, const char *Kt, const char *Vt, const TileAddr<T, D> &ad,
+                                           int kb, const uint4 (&q)[RowTile<T, D>::NS], float sl2, int lo, int hi) {
+  f32x16 s = tile_rows<T, D>(Kt, ad, kb, q, splat16(0.f));
+  dense_weights<D, MASKED>(st, s, sl2, lo, hi);
   tile_cols<D>(st.o, Vt, ad, kb, ColsOperand<T>(s));
+}
+
+// A column's result (weight sum l, reference m in log2 units) to o and lse, or to
+// its split's place. Rows that see nothing: 0 and -infinity.
+template <typename T, int D>
+__device__ __forceinline__ void dense_write(const DenseArgs &a, const DenseSlice &x, int s, int sp, int row, int tok,
+                                            int head, bool exists, bool valid, float l, float m, f32x16 (&o)[D / 32]) {
+  const bool some = valid && l > 0.f;
+  if (!some) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] = splat16(0.f);
+  }
+  const float inv = some ? 1.f / l : 0.f, lse2 = some ? __builtin_amdgcn_logf(l) + m : -INFINITY;
+  const bool first = exists && (threadIdx.x & 63) < 32;
+  if (a.splits == 1) {
+    store_column<D>((T *)(a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n), o, inv, exists);
+    if (a.lse && first) a.lse[((int64_t)x.b * a.H + head) * a.N + tok] = lse2 * 0.69314718055994531f;
+  } else {
+    const int64_t at = ((int64_t)s * a.R + row) * a.splits + sp;
+    store_column<D>(a.part_o + at * D, o, inv, exists);
+    if (first) a.part_lse[at] = lse2;
+  }
 }
 
 // Bound by the MFMA and VALU issue of long sequences (per score 4 D flops against
@@ -141,22 +169,119 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(
     compute(t + 1, lds1);
   }
 
-  const float l = column_sum(st.l);
-  const bool some = valid && l > 0.f;
-  const float inv = some ? 1.f / l : 0.f;
-  if (!some) {
+  dense_write<T, D>(a, x, s, sp, row, tok, head, exists, valid, column_sum(st.l), -st.nm, st.o);
+}
+
+// At most 32 rows per slice (single tokens): the four waves of a workgroup share
+// the rows and take the block's 32-key tiles in turn, each with tiles of its own
+// in LDS and no barrier, so that every wave streams keys. Bound by the bytes of K
+// and V: a wave refills its K tile while the values multiply and its V tile while
+// the next scores form. The waves' results are joined at the end by their
+// reference maxima.
+template <typename T, int D> struct FewTile {
+  using RT = RowTile<T, D>;
+  static constexpr int NW = 4, BYTES = 32 * RT::RB, NI = 32 / RT::RPI;  // copies per tile and wave
+};
+
+// The wave's next tile: rows past the last repeat it.
+template <typename T, int D>
+__device__ __forceinline__ void few_copy(char *tile, const char *base, int64_t first, uint32_t stride, int nrows) {
+  using RT = RowTile<T, D>;
+  const int lane = threadIdx.x & 63;
+  const char *src = base + first * (int64_t)stride;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) st.o[i] = splat16(0.f);
+  for (int j = 0; j < FewTile<T, D>::NI; ++j) {
+    const int r = j * RT::RPI + lane / RT::CPR;
+    copy16_unwaited(src + (uint32_t)min(r, nrows - 1) * stride + (uint32_t)(((lane % RT::CPR) ^ RT::swz(r)) << 4),
+                    tile + j * 1024);
   }
-  const float lse2 = some ? __builtin_amdgcn_logf(l) - st.nm : -INFINITY;
-  if (a.splits == 1) {
-    store_column<D>((T *)(a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n), st.o, inv, exists);
-    if (a.lse && exists && lane < 32) a.lse[((int64_t)x.b * a.H + head) * a.N + tok] = lse2 * 0.69314718055994531f;
-  } else {
-    const int64_t at = ((int64_t)s * a.R + row) * a.splits + sp;
-    store_column<D>(a.part_o + at * D, st.o, inv, exists);
-    if (exists && lane < 32) a.part_lse[at] = lse2;
+}
+
+template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_few_kernel(DenseArgs a) {
+  using RT = RowTile<T, D>;
+  using FT = FewTile<T, D>;
+  __shared__ __align__(16) char ldsK[FT::NW * FT::BYTES];
+  __shared__ __align__(16) char ldsV[FT::NW * FT::BYTES];
+  __shared__ float join_m[FT::NW][32], join_l[FT::NW][32];
+  int s, sp;
+  dense_block(blockIdx.x, a.B * a.Hkv, a.splits, s, sp);
+  const DenseSlice x = dense_slice(a, s);
+  const int lane = threadIdx.x & 63, n = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+
+  const int tok = div_group(a, n), head = x.hk * a.G + n - tok * a.G;
+  const bool exists = n < a.R, valid = exists && tok < x.qlen;
+  const int last = min(a.N, x.qlen) - 1;  // the last query (-1: none)
+  const int kbeg = first_key(a, x, 0), kend = last >= 0 ? end_key(a, x, last) : 0;
+  const int nt = kend > kbeg ? (kend - kbeg + 31) / 32 : 0;
+  const int per = (nt + a.splits - 1) / a.splits;
+  const int t1 = min(nt, (sp + 1) * per);
+  const char *kb = a.k.p + x.b * a.k.b + x.hk * a.k.h, *vb = a.v.p + x.b * a.v.b + x.hk * a.v.h;
+  char *Kt = ldsK + w * FT::BYTES, *Vt = ldsV + w * FT::BYTES;
+
+  uint4 q[RT::NS];
+  load_column<T, D>(q, a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
+  const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
+  // keys in [lo1, hi0) are seen by every query
+  const int lo1 = first_key(a, x, last), hi0 = end_key(a, x, 0);
+  TileAddr<T, D> ad;
+  ad.init();
+  DenseState<D> st;
+  st.init();
+  int t = sp * per + w;
+  if (t < t1) {
+    const int k0 = kbeg + 32 * t;
+    few_copy<T, D>(Kt, kb, k0, a.k.n, x.klen - k0);
+    few_copy<T, D>(Vt, vb, k0, a.v.n, x.klen - k0);
   }
+  wait_copies<0>();  // (the queries too: no wait for them inside the loop)
+  for (; t < t1; t += FT::NW) {
+    const int k0 = kbeg + 32 * t, k1 = k0 + 32 * FT::NW;
+    const bool more = t + FT::NW < t1;
+    wait_copies<FT::NI>();  // K is here, V may be in flight
+    f32x16 sc = tile_rows<T, D>(Kt, ad, 0, q, splat16(0.f));
+    wait_lds();  // and has been read
+    if (more) few_copy<T, D>(Kt, kb, k1, a.k.n, x.klen - k1);
+    if (k0 >= lo1 && k0 + 32 <= hi0)
+      dense_weights<D, false>(st, sc, a.sl2, 0, 0);
+    else
+      dense_weights<D, true>(st, sc, a.sl2, lo - k0, hi - k0);
+    if (more)
+      wait_copies<FT::NI>();  // V is here, the next K may be in flight
+    else
+      wait_copies<0>();
+    tile_cols<D>(st.o, Vt, ad, 0, ColsOperand<T>(sc));
+    wait_lds();
+    if (more) few_copy<T, D>(Vt, vb, k1, a.v.n, x.klen - k1);
+  }
+
+  // every wave's sums relative to the common maximum, added in pairs: waves 0 and
+  // 2, 1 and 3, then both (element e of a lane's accumulators at 64 e + lane)
+  const float l = column_sum(st.l);
+  if (lane < 32) join_m[w][n] = l > 0.f ? -st.nm : -INFINITY;
+  __syncthreads();  // (also: every wave is done with its tiles)
+  float m = join_m[0][n];
+#pragma unroll
+  for (int i = 1; i < FT::NW; ++i) m = fmaxf(m, join_m[i][n]);
+  const float f = l > 0.f ? __builtin_amdgcn_exp2f(-st.nm - m) : 0.f;
+  if (lane < 32) join_l[w][n] = l * f;
+  float *const jk = (float *)ldsK + lane, *const jv = (float *)ldsV + lane;
+  auto each = [&](auto &&op) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) st.o[i][e] = op(st.o[i][e], 16 * i + e);
+  };
+  each([&](float o, int) { return f > 0.f ? o * f : 0.f; });
+  if (w >= 2) each([&](float o, int e) { return jk[((w - 2) * (D / 2) + e) * 64] = o; });
+  __syncthreads();
+  if (w < 2) each([&](float o, int e) { return o + jk[(w * (D / 2) + e) * 64]; });
+  if (w == 1) each([&](float o, int e) { return jv[e * 64] = o; });
+  __syncthreads();
+  if (w >= 1) return;
+  each([&](float o, int e) { return o + jv[e * 64]; });
+  dense_write<T, D>(a, x, s, sp, n, tok, head, exists, valid, (join_l[0][n] + join_l[2][n]) + (join_l[1][n] + join_l[3][n]),
+                    m, st.o);
 }
 
 // Joins a row's splits by their log-sum-exps: D / 4 lanes per row.
@@ -225,8 +350,13 @@ DenseArgs dense_args(const mita_dense_cfg_t &c) {
 
 namespace {
 template <typename T, int D> hipError_t forward_t(const DenseArgs &a, hipStream_t st) {
-  dense_fwd_kernel<T, D><<<dim3((unsigned)(a.B * a.Hkv) * a.tiles * a.splits), 256, 0, st>>>(a);
-  hipError_t e = launched("dense_fwd_kernel", st);
+  const dim3 grid((unsigned)(a.B * a.Hkv) * a.tiles * a.splits);
+  const bool few = a.R <= DENSE_FEW;
+  if (few)
+    dense_few_kernel<T, D><<<grid, 256, 0, st>>>(a);
+  else
+    dense_fwd_kernel<T, D><<<grid, 256, 0, st>>>(a);
+  hipError_t e = launched(few ? "dense_few_kernel" : "dense_fwd_kernel", st);
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.R, per = 256 / (D / 4);
   dense_join_kernel<T, D><<<dim3((unsigned)((rows + per - 1) / per)), 256, 0, st>>>(a);

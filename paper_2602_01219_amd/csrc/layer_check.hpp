@@ -13,6 +13,7 @@
 namespace mita {
 
 constexpr int DENSE_TQ = 128;  // query rows of a dense attention workgroup (32 per wave)
+constexpr int DENSE_FEW = 32;   // rows per slice up to which a workgroup's waves share them
 constexpr int DENSE_KB = 128;  // keys of a key-side backward workgroup
 constexpr int CUS = 256;       // compute units of the MI355X
 constexpr int DENSE_MAX_SPLITS = 64;
@@ -207,6 +208,13 @@ inline DensePlan dense_plan(const mita_dense_cfg_t &c) {
   DensePlan p;
   p.tiles = (int)((dense_rows(c) + DENSE_TQ - 1) / DENSE_TQ);
   p.splits = splits_for(slices(c) * p.tiles, keys_seen(c), 512);
+  if (dense_rows(c) <= DENSE_FEW) {
+    // a few rows stream keys: just over two workgroups per CU (192 slices of up to
+    // 16384 keys, d = 128: 217 us; one per CU 234, four 229, eight 242, as every
+    // workgroup starts with nothing in flight), 256 keys each at least
+    const int64_t want = (2 * CUS) / slices(c) + 1;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, keys_seen(c) / 256, (int64_t)DENSE_MAX_SPLITS}));
+  }
   return p;
 }
 
@@ -331,10 +339,11 @@ inline NormPlan norm_plan(const mita_norm_cfg_t &c, bool vec) {
   const int ve = vec ? 16 / (int)elem_bytes(c) : 1;
   const int n = (c.C + ve - 1) / ve;  // pieces
   if (vec) {
-    for (int t = 8; t <= 64; t *= 2)
-      if (n <= t) return {ve, t, 1};
-    for (int p = 2; p <= 4; p *= 2)
-      if (n <= 64 * p) return {ve, 64, p};
+    // within a wave: the fewest idle lanes (768 bf16 elements: 32 threads of three
+    // pieces), then the fewest registers
+    static const int g[9][2] = {{8, 1}, {16, 1}, {32, 1}, {16, 3}, {64, 1}, {32, 3}, {64, 2}, {64, 3}, {64, 4}};
+    for (const auto &x : g)
+      if (n <= x[0] * x[1]) return {ve, x[0], x[1]};
     for (int p = 2; p <= 8; p *= 2)
       if (n <= 256 * p) return {ve, 256, p};
   } else {

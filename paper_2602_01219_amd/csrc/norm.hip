@@ -18,22 +18,32 @@ namespace mita {
 namespace {
 
 struct NormRows {
-  int64_t s[3];  // distances in elements
+  int64_t s[3];  // distances in elements, in the order of the walk
+  bool flat;     // rows of the walk are s[2] apart all over
 };
 struct NormArgs {
   const void *x, *dy, *w, *b;
   void *y, *dx, *dw, *db;
   const float *mean_in, *rstd_in;
   float *mean, *rstd, *part;
-  NormRows sx, sy, sdy, sdx;
+  // rows are walked in the order of x in memory, dimensions 0, 1, 2 from the
+  // outside in; `stat` is the place of the row's statistics
+  NormRows sx, sy, sdy, sdx, stat;
   int rows, n1, n2, C;
-  bool flat, w16;  // flat: rows are s[2] apart all over; w16: weights in bf16
+  uint32_t m1, m2;  // for quotients by n1 and n2
+  int h1, h2;
+  bool w16;  // weights in bf16
   float eps, invC;
 };
 
+// r / n for r < 2^31 with l = ceil(log2 n), m = 2^(31 + l) / n + 1 (floored, below
+// 2^32 + 1 and so below 2^32 for n > 1), h = l - 1: r m exceeds 2^(31 + l) r / n by
+// at most r < 2^31, less than a step of 1 / n. n = 1: h < 0.
+__device__ __forceinline__ int quotient(int r, uint32_t m, int h) { return h < 0 ? r : (int)(__umulhi((uint32_t)r, m) >> h); }
+
 __device__ __forceinline__ int64_t row_at(const NormArgs &a, const NormRows &s, int r) {
-  if (a.flat) return (int64_t)r * s.s[2];
-  const int i2 = r % a.n2, t = r / a.n2, i1 = t % a.n1, i0 = t / a.n1;
+  if (s.flat) return (int64_t)r * s.s[2];
+  const int t = quotient(r, a.m2, a.h2), i2 = r - t * a.n2, i0 = quotient(t, a.m1, a.h1), i1 = t - i0 * a.n1;
   return i0 * s.s[0] + i1 * s.s[1] + i2 * s.s[2];
 }
 
@@ -64,178 +74,208 @@ template <typename T, int VE> __device__ __forceinline__ void put(T *p, const fl
 
 template <typename T, int VE, int TPR, int P> struct RowRegs {
   Piece<T, VE> c[P];
-  __device__ __forceinline__ void load(const void *base, int64_t at, int C, int t, bool ok) {
+  // pieces past the row repeat its last one (see `get`)
+  __device__ __forceinline__ void load(const T *row, int C, int t) {
 #pragma unroll
-    for (int j = 0; j < P; ++j) {
-      const int i = (j * TPR + t) * VE;
-      if (ok && i < C)
-        c[j].load((const T *)base + at + i);
-      else
-        c[j].zero();
-    }
+    for (int j = 0; j < P; ++j) c[j].load(row + min((j * TPR + t) * VE, C - VE));
+  }
+  // piece j in fp32, zero past the row
+  __device__ __forceinline__ void get(float (&f)[VE], int j, int C, int t) const {
+    c[j].get(f);
+    const bool in = (j * TPR + t) * VE < C;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) f[e] = in ? f[e] : 0.f;
   }
 };
 
-// VE weights from column i on (`missing` where there are none).
-template <int VE> __device__ __forceinline__ void weights(float *f, const void *w, bool w16, int i, int C, float missing) {
+// The thread's weights (`missing` without any): column (j TPR + t) VE + e. Past the
+// row they repeat its last columns.
+template <int VE, int TPR, int P>
+__device__ __forceinline__ void weights(float (&f)[P][VE], const void *w, bool w16, int C, int t, float missing) {
+  if (!w) {
 #pragma unroll
-  for (int e = 0; e < VE; ++e) f[e] = missing;
-  if (!w || i >= C) return;
+    for (int j = 0; j < P; ++j)
 #pragma unroll
-  for (int e = 0; e < VE; ++e) f[e] = w16 ? to_f32(((const bf16_t *)w)[i + e]) : ((const float *)w)[i + e];
+      for (int e = 0; e < VE; ++e) f[j][e] = missing;
+  } else if (w16) {
+    uint16_t u[P][VE];
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) u[j][e] = ((const uint16_t *)w)[min((j * TPR + t) * VE, C - VE) + e];
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) f[j][e] = bf16_to_f32(u[j][e]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < P; ++j)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) f[j][e] = ((const float *)w)[min((j * TPR + t) * VE, C - VE) + e];
+  }
 }
 
-// Sum over the TPR threads of a row (the same in all of them). `red` is used in
-// turn by consecutive calls of a workgroup that shares a row.
-template <int TPR> __device__ __forceinline__ void row_sum2(float &x, float &y, float2 (*red)[4], int &turn) {
-  constexpr int W = TPR < 64 ? TPR : 64;
-#pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1) {
-    x += __shfl_xor(x, o);
-    y += __shfl_xor(y, o);
+// Sum over the lanes of a group of W (a power of two), the same in each: lanes are
+// paired within quads, halves and rows of 16 by DPP, then across rows by swaps.
+template <int W> __device__ __forceinline__ float group_sum(float x) {
+  auto dpp = [](float v, auto ctrl) {
+    return __uint_as_float(
+        (uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x += dpp(x, std::integral_constant<int, 0xb1>{});   // quad_perm 1 0 3 2
+  x += dpp(x, std::integral_constant<int, 0x4e>{});   // quad_perm 2 3 0 1
+  x += dpp(x, std::integral_constant<int, 0x141>{});  // row_half_mirror
+  if constexpr (W >= 16) x += dpp(x, std::integral_constant<int, 0x140>{});  // row_mirror
+  if constexpr (W >= 32) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
   }
+  if constexpr (W >= 64) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
+  return x;
+}
+
+// Sums over the TPR threads of a row. Those of a workgroup's four-wave parts go
+// through `red`, whose halves consecutive calls use in turn.
+template <int TPR, int K> __device__ __forceinline__ void row_sum(float (&x)[K], float (*red)[4][K], int &turn) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) x[k] = group_sum < TPR<64 ? TPR : 64>(x[k]);
   if constexpr (TPR > 64) {
-    const int sub = (threadIdx.x / TPR), w = (threadIdx.x % TPR) >> 6;
-    float2(*r)[4] = red + 4 * turn;
+    const int sub = threadIdx.x / TPR, w = (threadIdx.x % TPR) >> 6;
+    float(*r)[K] = red[4 * turn + sub];
     turn ^= 1;
-    if ((threadIdx.x & 63) == 0) r[sub][w] = make_float2(x, y);
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) r[w][k] = x[k];
+    }
     __syncthreads();
-    const float2 p0 = r[sub][0], p1 = r[sub][1], p2 = r[sub][2], p3 = r[sub][3];
-    x = (p0.x + p1.x) + (p2.x + p3.x);
-    y = (p0.y + p1.y) + (p2.y + p3.y);
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = (r[0][k] + r[1][k]) + (r[2][k] + r[3][k]);
   }
 }
 
-template <typename T, int VE, int TPR, int P>
+// U rows per thread group, all loaded before the first is reduced; a workgroup
+// does not go on to others: nothing would wait for its stores, but the next loads
+// would (loads and stores share one counter).
+template <typename T, int VE, int TPR, int P, int U>
 __global__ void __launch_bounds__(NORM_FWD_THREADS) norm_fwd_kernel(NormArgs a) {
   constexpr int RPB = NORM_FWD_THREADS / TPR;
-  __shared__ float2 red[8][4];
+  __shared__ float red[8][4][1];
   int turn = 0;
-  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  float w[P][VE], b[P][VE];
+  const int t = threadIdx.x % TPR, r0 = blockIdx.x * RPB * U + threadIdx.x / TPR;
+  RowRegs<T, VE, TPR, P> x[U];
 #pragma unroll
-  for (int j = 0; j < P; ++j) {
-    weights<VE>(w[j], a.w, a.w16, (j * TPR + t) * VE, a.C, 1.f);
-    weights<VE>(b[j], a.b, a.w16, (j * TPR + t) * VE, a.C, 0.f);
-  }
-  RowRegs<T, VE, TPR, P> next;
-  int r = blockIdx.x * RPB + sub;
-  next.load(a.x, row_at(a, a.sx, min(r, a.rows - 1)), a.C, t, r < a.rows);
-  // the loop is uniform over the workgroup: rows past the last are not written
-  for (int r0 = blockIdx.x * RPB; r0 < a.rows; r0 += gridDim.x * RPB) {
-    r = r0 + sub;
-    const RowRegs<T, VE, TPR, P> cur = next;
-    const int rn = r + gridDim.x * RPB;
-    if (r0 + gridDim.x * RPB < a.rows) next.load(a.x, row_at(a, a.sx, min(rn, a.rows - 1)), a.C, t, rn < a.rows);
-    float v[P][VE], sum = 0.f, none = 0.f;
+  for (int u = 0; u < U; ++u)
+    x[u].load((const T *)a.x + row_at(a, a.sx, min(r0 + u * RPB, a.rows - 1)), a.C, t);
+  float w[P][VE], b[P][VE];
+  weights<VE, TPR, P>(w, a.w, a.w16, a.C, t, 1.f);
+  weights<VE, TPR, P>(b, a.b, a.w16, a.C, t, 0.f);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = r0 + u * RPB;
+    float v[P][VE], sum[1] = {0.f};
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      cur.c[j].get(v[j]);
+      x[u].get(v[j], j, a.C, t);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) sum += v[j][e];
+      for (int e = 0; e < VE; ++e) sum[0] += v[j][e];
     }
-    row_sum2<TPR>(sum, none, red, turn);
-    const float mean = sum * a.invC;
-    float var = 0.f;
-    none = 0.f;
+    row_sum<TPR>(sum, red, turn);
+    const float mean = sum[0] * a.invC;
+    float var[1] = {0.f};
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       const bool in = (j * TPR + t) * VE < a.C;
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
         v[j][e] = in ? v[j][e] - mean : 0.f;
-        var += v[j][e] * v[j][e];
+        var[0] = __builtin_fmaf(v[j][e], v[j][e], var[0]);
       }
     }
-    row_sum2<TPR>(var, none, red, turn);
-    const float rstd = 1.f / sqrtf(var * a.invC + a.eps);
+    row_sum<TPR>(var, red, turn);
+    const float rstd = 1.f / sqrtf(var[0] * a.invC + a.eps);
     if (r < a.rows) {
-      const int64_t at = row_at(a, a.sy, r);
+      T *y = (T *)a.y + row_at(a, a.sy, r);
 #pragma unroll
       for (int j = 0; j < P; ++j) {
         const int i = (j * TPR + t) * VE;
-        float y[VE];
+        float o[VE];
 #pragma unroll
-        for (int e = 0; e < VE; ++e) y[e] = __builtin_fmaf(v[j][e] * rstd, w[j][e], b[j][e]);
-        if (i < a.C) put<T, VE>((T *)a.y + at + i, y);
+        for (int e = 0; e < VE; ++e) o[e] = __builtin_fmaf(v[j][e] * rstd, w[j][e], b[j][e]);
+        if (i < a.C) put<T, VE>(y + i, o);
       }
-      if (t == 0) {
-        if (a.mean) a.mean[r] = mean;
-        if (a.rstd) a.rstd[r] = rstd;
+      if (t == 0 && (a.mean || a.rstd)) {
+        const int64_t at = row_at(a, a.stat, r);
+        if (a.mean) a.mean[at] = mean;
+        if (a.rstd) a.rstd[at] = rstd;
       }
     }
   }
 }
 
-// WG: are dw and db wanted?
+// WG: are dw and db wanted? A workgroup goes over rows gridDim.x * RPB apart and
+// keeps its columns' sums.
 template <typename T, int VE, int TPR, int P, bool WG>
 __global__ void __launch_bounds__(NORM_BWD_THREADS) norm_bwd_kernel(NormArgs a) {
   constexpr int RPB = NORM_BWD_THREADS / TPR;
-  __shared__ float2 red[8][4];
+  __shared__ float red[8][4][2];
   __shared__ float sums[WG ? NORM_BWD_THREADS * VE : 1];
   int turn = 0;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float w[P][VE], dw[P][VE], db[P][VE];
+  weights<VE, TPR, P>(w, a.w, a.w16, a.C, t, 1.f);
 #pragma unroll
-  for (int j = 0; j < P; ++j) {
-    weights<VE>(w[j], a.w, a.w16, (j * TPR + t) * VE, a.C, 1.f);
+  for (int j = 0; j < P; ++j)
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
       dw[j][e] = 0.f;
       db[j][e] = 0.f;
     }
-  }
-  RowRegs<T, VE, TPR, P> nx, ny;
-  float nm, nr;
-  auto fetch = [&](int r) {
-    const int rc = min(r, a.rows - 1);
-    nx.load(a.x, row_at(a, a.sx, rc), a.C, t, r < a.rows);
-    ny.load(a.dy, row_at(a, a.sdy, rc), a.C, t, r < a.rows);
-    nm = a.mean_in[rc];
-    nr = a.rstd_in[rc];
-  };
-  fetch(blockIdx.x * RPB + sub);
+  // the loop is uniform over the workgroup: rows past the last weigh nothing
   for (int r0 = blockIdx.x * RPB; r0 < a.rows; r0 += gridDim.x * RPB) {
-    const int r = r0 + sub;
-    const RowRegs<T, VE, TPR, P> cx = nx, cy = ny;
-    const float mean = nm, rstd = nr;
-    if (r0 + gridDim.x * RPB < a.rows) fetch(r + gridDim.x * RPB);
-    float s1 = 0.f, s2 = 0.f;
+    const int r = r0 + sub, rc = min(r, a.rows - 1);
+    RowRegs<T, VE, TPR, P> x, y;
+    x.load((const T *)a.x + row_at(a, a.sx, rc), a.C, t);
+    y.load((const T *)a.dy + row_at(a, a.sdy, rc), a.C, t);
+    const int64_t at = row_at(a, a.stat, rc);
+    const float mean = a.mean_in[at], rstd = a.rstd_in[at], on = r < a.rows ? 1.f : 0.f;
+    float sm[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       float xv[VE], yv[VE];
-      cx.c[j].get(xv);
-      cy.c[j].get(yv);
+      x.c[j].get(xv);
+      y.get(yv, j, a.C, t);
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
         const float h = (xv[e] - mean) * rstd, gw = yv[e] * w[j][e];
-        // elements past the row, and rows past the last, have dy = 0
-        s1 += gw;
-        s2 = __builtin_fmaf(gw, h, s2);
+        // elements past the row have dy = 0
+        sm[0] += gw;
+        sm[1] = __builtin_fmaf(gw, h, sm[1]);
         if (WG) {
-          dw[j][e] = __builtin_fmaf(yv[e], h, dw[j][e]);
-          db[j][e] += yv[e];
+          dw[j][e] = __builtin_fmaf(yv[e] * on, h, dw[j][e]);
+          db[j][e] = __builtin_fmaf(yv[e], on, db[j][e]);
         }
       }
     }
     if (!a.dx) continue;
-    row_sum2<TPR>(s1, s2, red, turn);
-    s1 *= a.invC;
-    s2 *= a.invC;
+    row_sum<TPR>(sm, red, turn);
+    const float s1 = sm[0] * a.invC, s2 = sm[1] * a.invC;
     if (r < a.rows) {
-      const int64_t at = row_at(a, a.sdx, r);
+      T *dx = (T *)a.dx + row_at(a, a.sdx, r);
 #pragma unroll
       for (int j = 0; j < P; ++j) {
         const int i = (j * TPR + t) * VE;
         float xv[VE], yv[VE];
-        cx.c[j].get(xv);
-        cy.c[j].get(yv);
+        x.c[j].get(xv);
+        y.c[j].get(yv);
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
           const float h = (xv[e] - mean) * rstd;
           yv[e] = rstd * (__builtin_fmaf(yv[e], w[j][e], -s1) - h * s2);
         }
-        if (i < a.C) put<T, VE>((T *)a.dx + at + i, yv);
+        if (i < a.C) put<T, VE>(dx + i, yv);
       }
     }
   }
@@ -263,22 +303,22 @@ __global__ void __launch_bounds__(NORM_BWD_THREADS) norm_bwd_kernel(NormArgs a) 
   }
 }
 
-// dw and db: the workgroups' partial sums, eight interleaved sequences per column
-// added in a fixed order.
-__global__ void __launch_bounds__(256) norm_sum_kernel(NormArgs a, int parts) {
-  __shared__ float s[8][33];
+// dw and db: the workgroups' partial sums, sixteen interleaved sequences per
+// column added in a fixed order.
+__global__ void __launch_bounds__(512) norm_sum_kernel(NormArgs a, int parts) {
+  __shared__ float s[16][33];
   const int c = threadIdx.x & 31, q = threadIdx.x >> 5, i = blockIdx.x * 32 + c;
   float y = 0.f;
   if (i < 2 * a.C) {
-#pragma unroll 8
-    for (int p = q; p < parts; p += 8) y += a.part[(int64_t)p * 2 * a.C + i];
+#pragma unroll 16
+    for (int p = q; p < parts; p += 16) y += a.part[(int64_t)p * 2 * a.C + i];
   }
   s[q][c] = y;
   __syncthreads();
   if (q != 0 || i >= 2 * a.C) return;
   y = 0.f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) y += s[k][c];
+  for (int k = 0; k < 16; ++k) y += s[k][c];
   void *out = i < a.C ? a.dw : a.db;
   const int at = i < a.C ? i : i - a.C;
   if (!out) return;
@@ -319,8 +359,9 @@ template <typename T> __global__ void __launch_bounds__(512) norm_fwd_wide_kerne
       y[i] = from_f32<T>(__builtin_fmaf((to_f32(x[i]) - mean) * rstd, weight_at(a.w, a.w16, i, 1.f),
                                         weight_at(a.b, a.w16, i, 0.f)));
     if (threadIdx.x == 0) {
-      if (a.mean) a.mean[r] = mean;
-      if (a.rstd) a.rstd[r] = rstd;
+      const int64_t at = row_at(a, a.stat, r);
+      if (a.mean) a.mean[at] = mean;
+      if (a.rstd) a.rstd[at] = rstd;
     }
   }
 }
@@ -329,7 +370,8 @@ template <typename T> __global__ void __launch_bounds__(512) norm_dx_wide_kernel
   for (int r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T *x = (const T *)a.x + row_at(a, a.sx, r), *dy = (const T *)a.dy + row_at(a, a.sdy, r);
     T *dx = (T *)a.dx + row_at(a, a.sdx, r);
-    const float mean = a.mean_in[r], rstd = a.rstd_in[r];
+    const int64_t at = row_at(a, a.stat, r);
+    const float mean = a.mean_in[at], rstd = a.rstd_in[at];
     float s1 = 0.f, s2 = 0.f;
     for (int i = threadIdx.x; i < a.C; i += blockDim.x) {
       const float gw = to_f32(dy[i]) * weight_at(a.w, a.w16, i, 1.f);
@@ -351,9 +393,10 @@ template <typename T> __global__ void __launch_bounds__(512) norm_dw_wide_kernel
   float dw = 0.f, db = 0.f;
 #pragma unroll 4
   for (int r = blockIdx.y; r < a.rows; r += gridDim.y) {
+    const int64_t at = row_at(a, a.stat, r);
     const float x = to_f32(((const T *)a.x)[row_at(a, a.sx, r) + i]);
     const float dy = to_f32(((const T *)a.dy)[row_at(a, a.sdy, r) + i]);
-    dw = __builtin_fmaf(dy, (x - a.mean_in[r]) * a.rstd_in[r], dw);
+    dw = __builtin_fmaf(dy, (x - a.mean_in[at]) * a.rstd_in[at], dw);
     db += dy;
   }
   float *part = a.part + (int64_t)blockIdx.y * 2 * a.C;
@@ -369,28 +412,35 @@ bool row_vectors(const mita_norm_cfg_t &c, const Strided &s, const void *p) {
     if (s.n[i] > 1 && s.s[i] % ve != 0) return false;
   return true;
 }
-// rows one distance apart over all dimensions: the distance of row r is r * s[2]
-bool flatten(const Strided &s, NormRows &out) {
-  for (int i = 0; i < 3; ++i) out.s[i] = s.s[i];
-  int64_t d = 0, inner = 1;  // distance of the innermost dimension of more than one row
-  bool ok = true;
-  for (int i = 2; i >= 0; --i) {
-    if (s.n[i] == 1) continue;
-    if (inner == 1)
-      d = s.s[i];
-    else if (s.s[i] != d * inner)
-      ok = false;
-    inner *= s.n[i];
-  }
-  if (ok) out.s[2] = d;
-  return ok;
-}
-
-NormArgs norm_args(const mita_norm_cfg_t &c) {
+// The arguments of a call on `tensors` strided tensors, whose distances go to
+// `to`; the statistics come last. The walk goes over the dimensions in the order of
+// the first tensor's distances.
+NormArgs norm_args(const mita_norm_cfg_t &c, const Strided *t, int tensors, NormRows NormArgs::*const *to) {
   NormArgs a{};
+  const int64_t stat[3] = {(int64_t)c.n[1] * c.n[2], c.n[2], 1};
+  int order[3] = {0, 1, 2};  // dimensions of one row outermost
+  std::stable_sort(order, order + 3, [&](int x, int y) {
+    if ((c.n[x] == 1) != (c.n[y] == 1)) return c.n[x] == 1;
+    return c.n[x] > 1 && t[0].s[x] > t[0].s[y];
+  });
+  int64_t n[3];
+  for (int k = 0; k < 3; ++k) n[k] = c.n[order[k]];
+  for (int i = 0; i <= tensors; ++i) {
+    NormRows &r = i < tensors ? a.*to[i] : a.stat;
+    for (int k = 0; k < 3; ++k) r.s[k] = n[k] == 1 ? 0 : i < tensors ? t[i].s[order[k]] : stat[order[k]];
+    r.flat = (n[1] == 1 || r.s[1] == n[2] * r.s[2]) && (n[0] == 1 || r.s[0] == n[1] * n[2] * r.s[2]);
+  }
+  auto magic = [](int64_t d, uint32_t &m, int &h) {
+    int l = 0;
+    while (((int64_t)1 << l) < d) ++l;
+    h = l - 1;
+    m = d == 1 ? 0u : (uint32_t)(((uint64_t)1 << (31 + l)) / (uint64_t)d + 1);
+  };
+  a.n1 = (int)n[1];
+  a.n2 = (int)n[2];
+  magic(n[1], a.m1, a.h1);
+  magic(n[2], a.m2, a.h2);
   a.rows = (int)norm_rows(c);
-  a.n1 = c.n[1];
-  a.n2 = c.n[2];
   a.C = c.C;
   a.w16 = c.wdtype == MITA_BF16;
   a.eps = c.eps;
@@ -399,9 +449,12 @@ NormArgs norm_args(const mita_norm_cfg_t &c) {
 }
 
 template <typename T, int VE, int TPR, int P> hipError_t fwd_p(const NormArgs &a, hipStream_t st) {
-  constexpr int RPB = NORM_FWD_THREADS / TPR;
-  const int blocks = std::min((a.rows + RPB - 1) / RPB, 8 * CUS);
-  norm_fwd_kernel<T, VE, TPR, P><<<dim3((unsigned)blocks), NORM_FWD_THREADS, 0, st>>>(a);
+  // as many rows per thread as give four pieces, once that leaves eight workgroups per CU
+  constexpr int RPB = NORM_FWD_THREADS / TPR, U = P >= 4 ? 1 : P >= 2 ? 2 : 4;
+  if (U > 1 && a.rows >= RPB * U * 8 * CUS)
+    norm_fwd_kernel<T, VE, TPR, P, U><<<dim3((unsigned)((a.rows + RPB * U - 1) / (RPB * U))), NORM_FWD_THREADS, 0, st>>>(a);
+  else
+    norm_fwd_kernel<T, VE, TPR, P, 1><<<dim3((unsigned)((a.rows + RPB - 1) / RPB)), NORM_FWD_THREADS, 0, st>>>(a);
   return launched("norm_fwd_kernel", st);
 }
 template <typename T, int VE, int TPR, int P> hipError_t bwd_p(const NormArgs &a, int blocks, hipStream_t st) {
@@ -417,11 +470,12 @@ template <typename T, typename F> hipError_t with_plan(const NormPlan &p, F &&f)
   constexpr int V = 16 / (int)sizeof(T);
   if (p.ve > 1) {
     if (p.tpr == 8) return f.template run<V, 8, 1>();
-    if (p.tpr == 16) return f.template run<V, 16, 1>();
-    if (p.tpr == 32) return f.template run<V, 32, 1>();
+    if (p.tpr == 16) return p.p == 1 ? f.template run<V, 16, 1>() : f.template run<V, 16, 3>();
+    if (p.tpr == 32) return p.p == 1 ? f.template run<V, 32, 1>() : f.template run<V, 32, 3>();
     if (p.tpr == 64) {
       if (p.p == 1) return f.template run<V, 64, 1>();
       if (p.p == 2) return f.template run<V, 64, 2>();
+      if (p.p == 3) return f.template run<V, 64, 3>();
       return f.template run<V, 64, 4>();
     }
     if (p.p == 2) return f.template run<V, 256, 2>();
@@ -467,7 +521,7 @@ template <typename T> hipError_t backward_t(const NormArgs &a, const NormPlan &p
     }
   }
   if (!wg) return e;
-  norm_sum_kernel<<<dim3((unsigned)((2 * a.C + 31) / 32)), 256, 0, st>>>(a, blocks);
+  norm_sum_kernel<<<dim3((unsigned)((2 * a.C + 31) / 32)), 512, 0, st>>>(a, blocks);
   return launched("norm_sum_kernel", st);
 }
 
@@ -475,40 +529,25 @@ template <typename T> hipError_t backward_t(const NormArgs &a, const NormPlan &p
 
 hipError_t launch_norm_forward(const mita_norm_cfg_t &c, const void *x, const void *w, const void *b, void *y,
                                float *mean, float *rstd, hipStream_t st) {
-  NormArgs a = norm_args(c);
-  const Strided sx = strided_rows(c, c.x), sy = strided_rows(c, c.y);
-  const bool fx = flatten(sx, a.sx), fy = flatten(sy, a.sy);
-  a.flat = fx && fy;
-  if (!a.flat) {
-    for (int i = 0; i < 3; ++i) {
-      a.sx.s[i] = sx.s[i];
-      a.sy.s[i] = sy.s[i];
-    }
-  }
+  const Strided t[2] = {strided_rows(c, c.x), strided_rows(c, c.y)};
+  NormRows NormArgs::*const to[2] = {&NormArgs::sx, &NormArgs::sy};
+  NormArgs a = norm_args(c, t, 2, to);
   a.x = x;
   a.w = w;
   a.b = b;
   a.y = y;
   a.mean = mean;
   a.rstd = rstd;
-  const NormPlan p = norm_plan(c, row_vectors(c, sx, x) && row_vectors(c, sy, y));
+  const NormPlan p = norm_plan(c, row_vectors(c, t[0], x) && row_vectors(c, t[1], y));
   return c.dtype == MITA_F32 ? forward_t<float>(a, p, st) : forward_t<bf16_t>(a, p, st);
 }
 
 hipError_t launch_norm_backward(const mita_norm_cfg_t &c, const void *x, const void *w, const float *mean,
                                 const float *rstd, const void *dy, void *dx, void *dw, void *db, void *ws,
                                 hipStream_t st) {
-  NormArgs a = norm_args(c);
-  const Strided sx = strided_rows(c, c.x), sdy = strided_rows(c, c.dy), sdx = strided_rows(c, c.dx);
-  const bool fx = flatten(sx, a.sx), fy = flatten(sdy, a.sdy), fd = flatten(sdx, a.sdx);
-  a.flat = fx && fy && fd;
-  if (!a.flat) {
-    for (int i = 0; i < 3; ++i) {
-      a.sx.s[i] = sx.s[i];
-      a.sdy.s[i] = sdy.s[i];
-      a.sdx.s[i] = sdx.s[i];
-    }
-  }
+  const Strided t[3] = {strided_rows(c, c.x), strided_rows(c, c.dy), strided_rows(c, c.dx)};
+  NormRows NormArgs::*const to[3] = {&NormArgs::sx, &NormArgs::sdy, &NormArgs::sdx};
+  NormArgs a = norm_args(c, t, 3, to);
   a.x = x;
   a.w = w;
   a.mean_in = mean;
@@ -518,7 +557,7 @@ hipError_t launch_norm_backward(const mita_norm_cfg_t &c, const void *x, const v
   a.dw = dw;
   a.db = db;
   a.part = (float *)ws;
-  const NormPlan p = norm_plan(c, row_vectors(c, sx, x) && row_vectors(c, sdy, dy) && row_vectors(c, sdx, dx));
+  const NormPlan p = norm_plan(c, row_vectors(c, t[0], x) && row_vectors(c, t[1], dy) && row_vectors(c, t[2], dx));
   const int blocks = norm_bwd_blocks(c, p);
   return c.dtype == MITA_F32 ? backward_t<float>(a, p, blocks, st) : backward_t<bf16_t>(a, p, blocks, st);
 }

@@ -387,8 +387,15 @@ def attend(cfg: Config, q, q_lm, v_lm, k_x, v_x, perm, offsets, o=None, ws=None,
 # ---------------------------------------------------------------------------
 # Dense attention and layer norm
 # ---------------------------------------------------------------------------
+class _Planned:
+    """Keeps the plans of its calls (see _Plan) out of copies and pickles."""
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_plans"}
+
+
 @dataclass(frozen=True)
-class DenseConfig:
+class DenseConfig(_Planned):
     """Dense attention problem (mita_dense_cfg_t without the strides, which are
     the tensors' own). H_kv = 0 means H, N_k = 0 means N; a query at position p
     sees the keys p - left .. p + right (-1: no bound; right = 0: causal)."""
@@ -424,7 +431,7 @@ class DenseConfig:
 
 
 @dataclass(frozen=True)
-class NormConfig:
+class NormConfig(_Planned):
     """Layer norm of rows of C elements (mita_norm_cfg_t without the strides):
     rows is the shape in front of the last dimension, up to three dimensions."""
     rows: tuple
@@ -436,6 +443,14 @@ class NormConfig:
     @property
     def shape(self):
         return tuple(self.rows) + (self.C,)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == "f32" else torch.bfloat16
+
+    @property
+    def torch_wdtype(self):
+        return torch.float32 if self.wdtype == "f32" else torch.bfloat16
 
     def struct(self, **tensors) -> NormCfgStruct:
         if not 1 <= len(self.rows) <= 3:
@@ -504,19 +519,98 @@ def _lengths(t, name, B, device):
     return None if t is None else _packed(t, name, (B,), torch.int32, device)
 
 
-def _workspace(ws, need, device):
+class _Plan:
+    """What a call needs besides addresses, for one configuration and the shapes,
+    strides, types and devices of its tensors (never their addresses)."""
+    __slots__ = ("cfg", "ref", "need", "device", "index", "outs")
+
+    def __init__(self, struct, need, device, outs):
+        self.cfg, self.ref, self.need, self.device, self.index = struct, ctypes.byref(struct), need, device, device.index
+        self.outs = outs  # per output: (shape, strides, dtype)
+
+    def out(self, t, i):
+        return self.new(i) if t is None else t
+
+    def new(self, i):
+        shape, strides, dtype = self.outs[i]
+        return torch.empty_strided(shape, strides, dtype=dtype, device=self.device)
+
+
+def _like(t):
+    """(shape, strides, dtype) of an output beside t: tokens before heads in
+    memory where t has them so (a projection's layout), else contiguous."""
+    shape = tuple(t.shape)
+    if t.dim() == 4 and shape[1] > 1 and shape[2] > 1 and t.stride(1) < t.stride(2):
+        B, H, N, d = shape
+        return shape, (N * H * d, d, H * d, 1), t.dtype
+    return _dense(shape, t.dtype)
+
+
+def _dense(shape, dtype):
+    strides, n = [], 1
+    for x in reversed(shape):
+        strides.append(n)
+        n *= x
+    return tuple(shape), tuple(reversed(strides)), dtype
+
+
+def _place(given, like):
+    """A stand-in with the strides of an output: the given tensor or the one to come."""
+    return given if given is not None else torch.empty_strided(*like[:2], dtype=like[2], device="meta")
+
+
+def _signature(ts):
+    return tuple([None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in ts])
+
+
+def _plan_for(cfg, kind, ts, make):
+    """The call's plan: looked up by the tensors' signature, checked and made the
+    first time."""
+    plans = cfg.__dict__.get("_plans")
+    if plans is None:
+        plans = cfg.__dict__["_plans"] = {}
+    try:
+        key = (kind, _signature(ts))
+        plan = plans.get(key)
+    except AttributeError:
+        plan = key = None  # not a tensor: make() says so
+    if plan is None:
+        plan = make(cfg, *ts)
+        if len(plans) >= 1024:
+            plans.clear()
+        plans[key] = plan
+    return plan
+
+
+def _ws_for(plan, ws):
     if ws is None:
-        return (torch.empty(need, dtype=torch.uint8, device=device) if need else None), need
-    if not ws.is_cuda or ws.device != device or not ws.is_contiguous():
+        if not plan.need:
+            return None, None, 0
+        ws = torch.empty(plan.need, dtype=torch.uint8, device=plan.device)
+    elif ws.device != plan.device or not ws.is_contiguous():
         raise ValueError("ws must be a contiguous tensor on the tensors' device")
-    return ws, ws.numel() * ws.element_size()
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-def _stream_on(stream, device):
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    if s.device != device:
-        raise ValueError(f"the stream is on {s.device}, the tensors on {device}")
-    return ctypes.c_void_p(s.cuda_stream)
+def _call(plan, fn, args, stream):
+    """fn(cfg, *args, stream) with the tensors' device current."""
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(plan.index)
+    else:
+        if stream.device != plan.device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {plan.device}")
+        raw = stream.cuda_stream
+    if torch.cuda.current_device() == plan.index:
+        st = fn(plan.ref, *args, raw)
+    else:
+        with torch.cuda.device(plan.index):
+            st = fn(plan.ref, *args, raw)
+    if st != MITA_OK:
+        _check(st)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def dense_check(cfg: DenseConfig) -> int:
@@ -527,36 +621,39 @@ def dense_workspace_size(cfg: DenseConfig, which: int = WS_FORWARD) -> int:
     return int(load_library().mita_dense_workspace_size(ctypes.byref(cfg.struct()), which))
 
 
-def dense_forward(cfg: DenseConfig, q, k, v, q_len=None, k_len=None, o=None, lse=None, want_lse=True, ws=None,
-                  stream=None):
-    """Dense attention (mita_dense_forward): (o [B, H, N, d], lse [B, H, N] fp32
-    or None). q, k, v may be strided (their last dimension dense); q_len, k_len
-    are [B] int32 device tensors."""
-    lib = load_library()
+def _dense_forward_plan(cfg, q, k, v, q_len, k_len, o, lse):
     _tensor(q, "q", cfg.q_shape, cfg.torch_dtype, None)
     dev = q.device
     _tensor(k, "k", cfg.k_shape, cfg.torch_dtype, dev)
     _tensor(v, "v", cfg.k_shape, cfg.torch_dtype, dev)
     _lengths(q_len, "q_len", cfg.B, dev)
     _lengths(k_len, "k_len", cfg.B, dev)
-    with torch.cuda.device(dev):
-        o = _out_like(q) if o is None else _tensor(o, "o", cfg.q_shape, cfg.torch_dtype, dev)
-        if lse is None:
-            lse = torch.empty(cfg.q_shape[:3], dtype=torch.float32, device=dev) if want_lse else None
-        else:
-            _packed(lse, "lse", cfg.q_shape[:3], torch.float32, dev)
-        c = cfg.struct(q=q, k=k, v=v, o=o)
-        ws, nws = _workspace(ws, int(lib.mita_dense_workspace_size(ctypes.byref(c), WS_FORWARD)), dev)
-        _check(lib.mita_dense_forward(ctypes.byref(c), _p(q), _p(k), _p(v), _p(q_len), _p(k_len), _p(o), _p(lse),
-                                      _p(ws), nws, _stream_on(stream, dev)))
+    if o is not None:
+        _tensor(o, "o", cfg.q_shape, cfg.torch_dtype, dev)
+    if lse is not None:
+        _packed(lse, "lse", cfg.q_shape[:3], torch.float32, dev)
+    outs = (_like(q), _dense(cfg.q_shape[:3], torch.float32))
+    c = cfg.struct(q=q, k=k, v=v, o=_place(o, outs[0]))
+    return _Plan(c, int(load_library().mita_dense_workspace_size(ctypes.byref(c), WS_FORWARD)), dev, outs)
+
+
+def dense_forward(cfg: DenseConfig, q, k, v, q_len=None, k_len=None, o=None, lse=None, want_lse=True, ws=None,
+                  stream=None):
+    """Dense attention (mita_dense_forward): (o [B, H, N, d], lse [B, H, N] fp32
+    or None). q, k, v may be strided (their last dimension dense); q_len, k_len
+    are [B] int32 device tensors."""
+    lib = load_library()
+    plan = _plan_for(cfg, "forward", (q, k, v, q_len, k_len, o, lse), _dense_forward_plan)
+    o = plan.out(o, 0)
+    if lse is None and want_lse:
+        lse = plan.new(1)
+    ws, wp, wn = _ws_for(plan, ws)
+    _call(plan, lib.mita_dense_forward, (q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_len), _ptr(k_len),
+                                         o.data_ptr(), _ptr(lse), wp, wn), stream)
     return o, lse
 
 
-def dense_backward(cfg: DenseConfig, q, k, v, o, lse, dO, q_len=None, k_len=None, dq=None, dk=None, dv=None, ws=None,
-                   stream=None):
-    """Gradients (dq, dk, dv) of dense_forward's o for the upstream gradient dO
-    (mita_dense_backward)."""
-    lib = load_library()
+def _dense_backward_plan(cfg, q, k, v, o, lse, dO, q_len, k_len, dq, dk, dv):
     _tensor(q, "q", cfg.q_shape, cfg.torch_dtype, None)
     dev, dt = q.device, cfg.torch_dtype
     for t, name, shape in ((k, "k", cfg.k_shape), (v, "v", cfg.k_shape), (o, "o", cfg.q_shape),
@@ -565,24 +662,26 @@ def dense_backward(cfg: DenseConfig, q, k, v, o, lse, dO, q_len=None, k_len=None
     _packed(lse, "lse", cfg.q_shape[:3], torch.float32, dev)
     _lengths(q_len, "q_len", cfg.B, dev)
     _lengths(k_len, "k_len", cfg.B, dev)
-    with torch.cuda.device(dev):
-        dq = _out_like(q) if dq is None else _tensor(dq, "dq", cfg.q_shape, dt, dev)
-        dk = _out_like(k) if dk is None else _tensor(dk, "dk", cfg.k_shape, dt, dev)
-        dv = _out_like(v) if dv is None else _tensor(dv, "dv", cfg.k_shape, dt, dev)
-        c = cfg.struct(q=q, k=k, v=v, o=o, dO=dO, dq=dq, dk=dk, dv=dv)
-        ws, nws = _workspace(ws, int(lib.mita_dense_workspace_size(ctypes.byref(c), WS_BACKWARD)), dev)
-        _check(lib.mita_dense_backward(ctypes.byref(c), _p(q), _p(k), _p(v), _p(o), _p(lse), _p(dO), _p(q_len),
-                                       _p(k_len), _p(dq), _p(dk), _p(dv), _p(ws), nws, _stream_on(stream, dev)))
+    for t, name, shape in ((dq, "dq", cfg.q_shape), (dk, "dk", cfg.k_shape), (dv, "dv", cfg.k_shape)):
+        if t is not None:
+            _tensor(t, name, shape, dt, dev)
+    outs = (_like(q), _like(k), _like(v))
+    c = cfg.struct(q=q, k=k, v=v, o=o, dO=dO, dq=_place(dq, outs[0]), dk=_place(dk, outs[1]), dv=_place(dv, outs[2]))
+    return _Plan(c, int(load_library().mita_dense_workspace_size(ctypes.byref(c), WS_BACKWARD)), dev, outs)
+
+
+def dense_backward(cfg: DenseConfig, q, k, v, o, lse, dO, q_len=None, k_len=None, dq=None, dk=None, dv=None, ws=None,
+                   stream=None):
+    """Gradients (dq, dk, dv) of dense_forward's o for the upstream gradient dO
+    (mita_dense_backward)."""
+    lib = load_library()
+    plan = _plan_for(cfg, "backward", (q, k, v, o, lse, dO, q_len, k_len, dq, dk, dv), _dense_backward_plan)
+    dq, dk, dv = plan.out(dq, 0), plan.out(dk, 1), plan.out(dv, 2)
+    ws, wp, wn = _ws_for(plan, ws)
+    _call(plan, lib.mita_dense_backward, (q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+                                          dO.data_ptr(), _ptr(q_len), _ptr(k_len), dq.data_ptr(), dk.data_ptr(),
+                                          dv.data_ptr(), wp, wn), stream)
     return dq, dk, dv
-
-
-def _out_like(t):
-    """A tensor for an output beside t: tokens before heads in memory where t has
-    them so (a projection's layout), else contiguous."""
-    if t.dim() == 4 and t.shape[1] > 1 and t.shape[2] > 1 and t.stride(1) < t.stride(2):
-        B, H, N, d = t.shape
-        return torch.empty((B, N, H, d), dtype=t.dtype, device=t.device).transpose(1, 2)
-    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def norm_check(cfg: NormConfig) -> int:
@@ -594,35 +693,49 @@ def norm_workspace_size(cfg: NormConfig) -> int:
     return int(load_library().mita_norm_workspace_size(ctypes.byref(cfg.struct())))
 
 
-def _norm_types(cfg):
-    return (torch.float32 if cfg.dtype == "f32" else torch.bfloat16,
-            torch.float32 if cfg.wdtype == "f32" else torch.bfloat16)
+def _norm_forward_plan(cfg, x, w, b, y, mean, rstd):
+    dt, wt = cfg.torch_dtype, cfg.torch_wdtype
+    _tensor(x, "x", cfg.shape, dt, None)
+    dev = x.device
+    for t, name in ((w, "w"), (b, "b")):
+        if t is not None:
+            _packed(t, name, (cfg.C,), wt, dev)
+    if y is not None:
+        _tensor(y, "y", cfg.shape, dt, dev)
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if t is not None:
+            _packed(t, name, cfg.rows, torch.float32, dev)
+    outs = (_like(x), _dense(cfg.rows, torch.float32))
+    return _Plan(cfg.struct(x=x, y=_place(y, outs[0])), 0, dev, outs)
 
 
 def norm_forward(cfg: NormConfig, x, w=None, b=None, y=None, mean=None, rstd=None, want_stats=True, stream=None):
     """Layer norm (mita_norm_forward): (y like x, mean and rstd [rows] fp32 or
     None). x may be strided (its last dimension dense)."""
     lib = load_library()
-    dt, wt = _norm_types(cfg)
+    plan = _plan_for(cfg, "forward", (x, w, b, y, mean, rstd), _norm_forward_plan)
+    y = plan.out(y, 0)
+    if want_stats:
+        mean, rstd = plan.out(mean, 1), plan.out(rstd, 1)
+    _call(plan, lib.mita_norm_forward, (x.data_ptr(), _ptr(w), _ptr(b), y.data_ptr(), _ptr(mean), _ptr(rstd)), stream)
+    return y, mean, rstd
+
+
+def _norm_backward_plan(cfg, x, mean, rstd, dy, w, dx, dw, db):
+    dt, wt = cfg.torch_dtype, cfg.torch_wdtype
     _tensor(x, "x", cfg.shape, dt, None)
     dev = x.device
-    for t, name in ((w, "w"), (b, "b")):
+    _tensor(dy, "dy", cfg.shape, dt, dev)
+    _packed(mean, "mean", cfg.rows, torch.float32, dev)
+    _packed(rstd, "rstd", cfg.rows, torch.float32, dev)
+    if dx is not None:
+        _tensor(dx, "dx", cfg.shape, dt, dev)
+    for t, name in ((w, "w"), (dw, "dw"), (db, "db")):
         if t is not None:
             _packed(t, name, (cfg.C,), wt, dev)
-    with torch.cuda.device(dev):
-        y = _out_like(x) if y is None else _tensor(y, "y", cfg.shape, dt, dev)
-        stats = []
-        for t, name in ((mean, "mean"), (rstd, "rstd")):
-            if t is None:
-                t = torch.empty(tuple(cfg.rows), dtype=torch.float32, device=dev) if want_stats else None
-            else:
-                _packed(t, name, cfg.rows, torch.float32, dev)
-            stats.append(t)
-        mean, rstd = stats
-        c = cfg.struct(x=x, y=y)
-        _check(lib.mita_norm_forward(ctypes.byref(c), _p(x), _p(w), _p(b), _p(y), _p(mean), _p(rstd),
-                                     _stream_on(stream, dev)))
-    return y, mean, rstd
+    outs = (_like(x), _dense((cfg.C,), wt))
+    c = cfg.struct(x=x, dy=dy, dx=_place(dx, outs[0]))
+    return _Plan(c, int(load_library().mita_norm_workspace_size(ctypes.byref(c))), dev, outs)
 
 
 def norm_backward(cfg: NormConfig, x, mean, rstd, dy, w=None, dx=None, dw=None, db=None, want_dx=True,
@@ -630,32 +743,14 @@ def norm_backward(cfg: NormConfig, x, mean, rstd, dy, w=None, dx=None, dw=None, 
     """Gradients (dx, dw, db) of norm_forward (mita_norm_backward); dx, or dw and
     db, are None unless wanted."""
     lib = load_library()
-    dt, wt = _norm_types(cfg)
-    _tensor(x, "x", cfg.shape, dt, None)
-    dev = x.device
-    _tensor(dy, "dy", cfg.shape, dt, dev)
-    _packed(mean, "mean", cfg.rows, torch.float32, dev)
-    _packed(rstd, "rstd", cfg.rows, torch.float32, dev)
-    if w is not None:
-        _packed(w, "w", (cfg.C,), wt, dev)
-    with torch.cuda.device(dev):
-        if dx is not None:
-            _tensor(dx, "dx", cfg.shape, dt, dev)
-        elif want_dx:
-            dx = _out_like(x)
-        grads = []
-        for t, name in ((dw, "dw"), (db, "db")):
-            if t is None:
-                t = torch.empty(cfg.C, dtype=wt, device=dev) if want_weights else None
-            else:
-                _packed(t, name, (cfg.C,), wt, dev)
-            grads.append(t)
-        dw, db = grads
-        c = cfg.struct(x=x, dy=dy, **({"dx": dx} if dx is not None else {}))
-        need = int(lib.mita_norm_workspace_size(ctypes.byref(c))) if dw is not None or db is not None else 0
-        ws, nws = _workspace(ws, need, dev)
-        _check(lib.mita_norm_backward(ctypes.byref(c), _p(x), _p(w), _p(mean), _p(rstd), _p(dy), _p(dx), _p(dw), _p(db),
-                                      _p(ws), nws, _stream_on(stream, dev)))
+    plan = _plan_for(cfg, "backward", (x, mean, rstd, dy, w, dx, dw, db), _norm_backward_plan)
+    if want_dx:
+        dx = plan.out(dx, 0)
+    if want_weights:
+        dw, db = plan.out(dw, 1), plan.out(db, 1)
+    ws, wp, wn = _ws_for(plan, ws) if dw is not None or db is not None else (None, None, 0)
+    _call(plan, lib.mita_norm_backward, (x.data_ptr(), _ptr(w), mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(),
+                                         _ptr(dx), _ptr(dw), _ptr(db), wp, wn), stream)
     return dx, dw, db
 
 
