@@ -58,10 +58,11 @@ __device__ __forceinline__ void copy4(const void *src, char *dst) {
 
 // The same copy without the waits that the compiler sets before LDS reads that it
 // cannot tell apart from it (it waits for every copy in flight where control flow
-// meets): the caller waits with wait_copies. dst is the same for the whole wave.
-__device__ __forceinline__ void copy16_unwaited(const void *src, char *dst) {
-  const uint32_t at = (uint32_t)(uintptr_t)(lds_void_t *)dst;
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(at) : "memory");
+// meets): the caller waits with wait_copies or tile_barrier. base and dst are the
+// same for the whole wave, off the lane's bytes behind base.
+__device__ __forceinline__ void copy16_unwaited(const char *base, uint32_t off, char *dst) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t *)dst);
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(at) : "memory");
 }
 
 // The copies this wave issued have landed, and those of every wave once all are
@@ -110,11 +111,35 @@ template <typename T, int D, int NW> struct TileCopy {
   __device__ __forceinline__ void issue(char *tile, const char *base, int64_t first, uint32_t stride,
                                         int nrows) const {
     const char *src = base + first * (int64_t)stride;
+    if (nrows >= RT::TR) {
 #pragma unroll
-    for (int j = 0; j < PW; ++j) {
-      const uint32_t o = nrows >= RT::TR ? off[j] : min(row[j], (uint32_t)(nrows - 1)) * stride + chunk[j];
-      copy16(src + o, tile + (w * PW + j) * 1024);
+      for (int j = 0; j < PW; ++j) copy16_unwaited(src, off[j], tile + (w * PW + j) * 1024);
+    } else {
+#pragma unroll
+      for (int j = 0; j < PW; ++j)
+        copy16_unwaited(src, min(row[j], (uint32_t)(nrows - 1)) * stride + chunk[j], tile + (w * PW + j) * 1024);
     }
+  }
+};
+
+// The tiles of a workgroup in the order it takes them: position p < nfull is tile
+// f0 + p, seen whole by every row; the others (which the window or an end cuts)
+// follow, those in front of the full ones first.
+struct TileOrder {
+  int f0, nfull, h0, nhead, r0, total;
+  // tiles [t0, t1), of which [f0, f1) are seen whole
+  __device__ __forceinline__ TileOrder(int t0, int t1, int fa, int fb) {
+    const int f1 = max(t0, min(fb, t1));
+    f0 = min(max(fa, t0), f1);
+    nfull = f1 - f0;
+    h0 = t0;
+    nhead = f0 - t0;
+    r0 = f1;
+    total = max(0, t1 - t0);
+  }
+  __device__ __forceinline__ int at(int p) const {
+    const int m = p - nfull;
+    return m < 0 ? f0 + p : m < nhead ? h0 + m : r0 + m - nhead;
   }
 };
 

@@ -25,23 +25,22 @@ template <int D> struct DenseState {
   }
 };
 
-// The online softmax of 32 scores: s becomes the weights. lo and hi bound the
-// column's visible keys, counted from the block's first.
-template <int D, bool MASKED>
-__device__ __forceinline__ void dense_weights(DenseState<D> &st, f32x16 &s, float sl2, int lo, int hi) {
+// Scores hidden from the column become -infinity: keys j of the 32 outside [lo, hi).
+__device__ __forceinline__ void dense_mask(f32x16 &s, int lo, int hi) {
   const int g = (threadIdx.x & 63) >> 5;
-  if (MASKED) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int j = acc_row(i, g);
-      s[i] = j >= lo && j < hi ? s[i] : -INFINITY;
-    }
+  for (int i = 0; i < 16; ++i) {
+    const int j = acc_row(i, g);
+    s[i] = j >= lo && j < hi ? s[i] : -INFINITY;
   }
+}
+
+// The reference moves only where a score passes it by more than RESCALE_LOG2 (and
+// at the column's first visible key): any reference gives the same softmax.
+template <int D> __device__ __forceinline__ void dense_reference(DenseState<D> &st, const f32x16 &s, float sl2) {
   float mx = s[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-  // the reference moves only where a score passes it by more than RESCALE_LOG2
-  // (and at the column's first visible key): any reference gives the same softmax
   if (__ballot(mx > st.thr)) {
     const float cm = column_max(mx);
     const bool up = cm > st.thr;
@@ -53,20 +52,17 @@ __device__ __forceinline__ void dense_weights(DenseState<D> &st, f32x16 &s, floa
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) st.o[i] *= alpha;
   }
+}
+
+// s becomes the weights exp2(s sl2 - m), which are added up.
+template <int D> __device__ __forceinline__ void dense_weights(DenseState<D> &st, f32x16 &s, float sl2) {
+  float l[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], sl2, st.nm));
-    st.l += s[i];
+    l[i & 1] += s[i];
   }
-}
-
-// 32 keys of a staged tile (rows 32 kb ..): scores, online softmax, values.
-template <typename T, int D, bool MASKED>
-__device__ __forceinline__ void dense_step(DenseState<D> &st, const char *Kt, const char *Vt, const TileAddr<T, D> &ad,
-                                           int kb, const uint4 (&q)[RowTile<T, D>::NS], float sl2, int lo, int hi) {
-  f32x16 s = tile_rows<T, D>(Kt, ad, kb, q, splat16(0.f));
-  dense_weights<D, MASKED>(st, s, sl2, lo, hi);
-  tile_cols<D>(st.o, Vt, ad, kb, ColsOperand<T>(s));
+  st.l += l[0] + l[1];
 }
 
 // A column's result (weight sum l, reference m in log2 units) to o and lse, or to
@@ -92,21 +88,48 @@ __device__ __forceinline__ void dense_write(const DenseArgs &a, const DenseSlice
 }
 
 // Bound by the MFMA and VALU issue of long sequences (per score 4 D flops against
-// one exp2, a quarter-rate instruction, and about three full-rate ones); by the
-// bytes of K and V for few rows, where `splits` workgroups share a tile's keys.
+// one exp2, a quarter-rate instruction, and about three full-rate ones). A wave
+// forms the scores of the next tile while it weighs the present one, so that its
+// MFMAs have VALU work to run beside, and two waves share a SIMD.
 template <typename T, int D>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(DenseArgs a) {
   using RT = RowTile<T, D>;
-  constexpr int TR = RT::TR;
-  __shared__ __align__(16) char lds0[2 * TR * RT::RB];
-  __shared__ __align__(16) char lds1[2 * TR * RT::RB];
+  constexpr int TR = RT::TR, HT = TR / 32, BYTES = TR * RT::RB;
+  __shared__ __align__(16) char ldsK[2 * BYTES];
+  __shared__ __align__(16) char ldsV[2 * BYTES];
   int s, item;
   dense_block(blockIdx.x, a.B * a.Hkv, a.tiles * a.splits, s, item);
   const int sp = item % a.splits;
   const int tile = a.tiles - 1 - item / a.splits;  // causal: the longest first
   const DenseSlice x = dense_slice(a, s);
-  const int lane = threadIdx.x & 63, n = lane & 31;
+  const int n = threadIdx.x & 31;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+
+  // the keys of the block
+  const int b0 = div_group(a, tile * DENSE_TQ);
+  const int b1 = min(div_group(a, min(tile * DENSE_TQ + DENSE_TQ, a.R) - 1), x.qlen - 1);
+  const int kbeg = first_key(a, x, b0), kend = b0 <= b1 ? end_key(a, x, b1) : 0;
+  const int nt = kend > kbeg ? (kend - kbeg + TR - 1) / TR : 0;
+  const int per = (nt + a.splits - 1) / a.splits;
+  const int t0 = sp * per, t1 = min(nt, t0 + per);
+  // of these, tiles that every row sees whole: keys [first_key(b1), end_key(b0))
+  const TileOrder order(t0, t1, (first_key(a, x, b1) - kbeg + TR - 1) / TR, max(0, end_key(a, x, b0) - kbeg) / TR);
+
+  TileAddr<T, D> ad;
+  ad.init();
+  TileCopy<T, D, 4> ck, cv;
+  ck.init(a.k.n);
+  cv.init(a.v.n);
+  const char *kb = a.k.p + x.b * a.k.b + x.hk * a.k.h, *vb = a.v.p + x.b * a.v.b + x.hk * a.v.h;
+  auto issue_k = [&](int p) {
+    const int k0 = kbeg + order.at(p) * TR;
+    ck.issue(ldsK + (p & 1) * BYTES, kb, k0, a.k.n, x.klen - k0);
+  };
+  auto issue_v = [&](int p) {
+    const int k0 = kbeg + order.at(p) * TR;
+    cv.issue(ldsV + (p & 1) * BYTES, vb, k0, a.v.n, x.klen - k0);
+  };
+  if (order.total > 0) issue_k(0);
 
   // the lane's row
   const int row = tile * DENSE_TQ + 32 * w + n;
@@ -115,60 +138,37 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(
   uint4 q[RT::NS];
   load_column<T, D>(q, a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
   const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
-
-  // the keys of the block and of the wave
-  const int b0 = div_group(a, tile * DENSE_TQ);
-  const int b1 = min(div_group(a, min(tile * DENSE_TQ + DENSE_TQ, a.R) - 1), x.qlen - 1);
-  const int kbeg = first_key(a, x, b0), kend = b0 <= b1 ? end_key(a, x, b1) : 0;
-  const int nt = kend > kbeg ? (kend - kbeg + TR - 1) / TR : 0;
-  const int per = (nt + a.splits - 1) / a.splits;
-  const int t0 = sp * per, t1 = min(nt, t0 + per);
-  const int wr = tile * DENSE_TQ + 32 * w;
-  const int w0 = wr < a.R ? div_group(a, wr) : x.qlen;
-  const int w1 = min(div_group(a, min(wr + 32, a.R) - 1), x.qlen - 1);
-  const bool busy = w0 <= w1;
-  const int lo0 = first_key(a, x, w0), lo1 = first_key(a, x, w1), hi0 = end_key(a, x, w0), hi1 = end_key(a, x, w1);
-
-  TileAddr<T, D> ad;
-  ad.init();
-  TileCopy<T, D, 4> ck, cv;
-  ck.init(a.k.n);
-  cv.init(a.v.n);
-  const char *kb = a.k.p + x.b * a.k.b + x.hk * a.k.h, *vb = a.v.p + x.b * a.v.b + x.hk * a.v.h;
   DenseState<D> st;
   st.init();
 
-  auto issue = [&](int t, char *buf) {
-    const int k0 = kbeg + t * TR;
-    ck.issue(buf, kb, k0, a.k.n, x.klen - k0);
-    cv.issue(buf + TR * RT::RB, vb, k0, a.v.n, x.klen - k0);
-  };
-  auto compute = [&](int t, const char *buf) {
-    const int k0 = kbeg + t * TR;
-    if (!busy) return;
+  f32x16 sc[HT];
+  auto scores = [&](int p, int h) { return tile_rows<T, D>(ldsK + (p & 1) * BYTES, ad, h, q, splat16(0.f)); };
+  auto tiles = [&](int p, int end, auto masked) {
+    for (; p < end; ++p) {
+      tile_barrier();
+      if (p + 2 < order.total) issue_k(p + 2);
+      if (p + 1 < order.total) issue_v(p + 1);
+      const int k0 = kbeg + order.at(p) * TR;
 #pragma unroll
-    for (int h = 0; h < TR / 32; ++h) {
-      const int kh = k0 + 32 * h;
-      if (kh >= hi1 || kh + 32 <= lo0) continue;
-      if (kh >= lo1 && kh + 32 <= hi0)
-        dense_step<T, D, false>(st, buf, buf + TR * RT::RB, ad, h, q, a.sl2, 0, 0);
-      else
-        dense_step<T, D, true>(st, buf, buf + TR * RT::RB, ad, h, q, a.sl2, lo - kh, hi - kh);
+      for (int h = 0; h < HT; ++h) {
+        f32x16 now = sc[h];
+        if (decltype(masked)::value) dense_mask(now, lo - k0 - 32 * h, hi - k0 - 32 * h);
+        dense_reference<D>(st, now, a.sl2);
+        sc[h] = scores(p + 1, h);  // (past the last tile: unused)
+        dense_weights<D>(st, now, a.sl2);
+        tile_cols<D>(st.o, ldsV + (p & 1) * BYTES, ad, h, ColsOperand<T>(now));
+      }
     }
   };
-  // two buffers as objects of their own: the compiler can tell the copies in
-  // flight from the tile being read
-  if (t0 < t1) issue(t0, lds0);
-  for (int t = t0; t < t1; t += 2) {
+  if (order.total > 0) {
     tile_barrier();
-    if (t + 1 < t1) issue(t + 1, lds1);
-    compute(t, lds0);
-    if (t + 1 >= t1) break;
-    tile_barrier();
-    if (t + 2 < t1) issue(t + 2, lds0);
-    compute(t + 1, lds1);
+    if (order.total > 1) issue_k(1);
+    issue_v(0);
+#pragma unroll
+    for (int h = 0; h < HT; ++h) sc[h] = scores(0, h);
+    tiles(0, order.nfull, std::false_type{});
+    tiles(order.nfull, order.total, std::true_type{});
   }
-
   dense_write<T, D>(a, x, s, sp, row, tok, head, exists, valid, column_sum(st.l), -st.nm, st.o);
 }
 
@@ -192,7 +192,7 @@ __device__ __forceinline__ void few_copy(char *tile, const char *base, int64_t f
 #pragma unroll
   for (int j = 0; j < FewTile<T, D>::NI; ++j) {
     const int r = j * RT::RPI + lane / RT::CPR;
-    copy16_unwaited(src + (uint32_t)min(r, nrows - 1) * stride + (uint32_t)(((lane % RT::CPR) ^ RT::swz(r)) << 4),
+    copy16_unwaited(src, (uint32_t)min(r, nrows - 1) * stride + (uint32_t)(((lane % RT::CPR) ^ RT::swz(r)) << 4),
                     tile + j * 1024);
   }
 }
@@ -242,10 +242,9 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) ==
     f32x16 sc = tile_rows<T, D>(Kt, ad, 0, q, splat16(0.f));
     wait_lds();  // and has been read
     if (more) few_copy<T, D>(Kt, kb, k1, a.k.n, x.klen - k1);
-    if (k0 >= lo1 && k0 + 32 <= hi0)
-      dense_weights<D, false>(st, sc, a.sl2, 0, 0);
-    else
-      dense_weights<D, true>(st, sc, a.sl2, lo - k0, hi - k0);
+    if (!(k0 >= lo1 && k0 + 32 <= hi0)) dense_mask(sc, lo - k0, hi - k0);
+    dense_reference<D>(st, sc, a.sl2);
+    dense_weights<D>(st, sc, a.sl2);
     if (more)
       wait_copies<FT::NI>();  // V is here, the next K may be in flight
     else
