@@ -48,21 +48,23 @@ template <typename T, int D> struct RowTile {
   }
 };
 
-// LDS DMA of 16 (4) bytes per lane: lane l's go to dst + 16 l (4 l).
-__device__ __forceinline__ void copy16(const void *src, char *dst) {
-  __builtin_amdgcn_global_load_lds(src, (lds_void_t *)dst, 16, 0, 0);
+// LDS DMA of 16 (4) bytes per lane: lane l's go to LDS address at + 16 l (4 l). Written as
+// instructions because around the builtin the compiler sets waits of its own before
+// LDS reads that it cannot tell apart from the copy (for every copy in flight, where
+// control flow meets): the caller waits with wait_copies or tile_barrier. base and
+// at are the same for the whole wave, off the lane's bytes behind base.
+__device__ __forceinline__ uint32_t lds_at(char *p) {  // address of the workgroup's LDS
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t *)p);
 }
-__device__ __forceinline__ void copy4(const void *src, char *dst) {
-  __builtin_amdgcn_global_load_lds(src, (lds_void_t *)dst, 4, 0, 0);
+__device__ __forceinline__ void copy16_unwaited(const char *base, uint32_t off, uint32_t at) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(at) : "memory");
 }
 
-// The same copy without the waits that the compiler sets before LDS reads that it
-// cannot tell apart from it (it waits for every copy in flight where control flow
-// meets): the caller waits with wait_copies or tile_barrier. base and dst are the
-// same for the whole wave, off the lane's bytes behind base.
-__device__ __forceinline__ void copy16_unwaited(const char *base, uint32_t off, char *dst) {
-  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t *)dst);
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(at) : "memory");
+__device__ __forceinline__ void copy16_unwaited(const char *src, uint32_t at) {  // any 64-bit address per lane
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(at) : "memory");
+}
+__device__ __forceinline__ void copy4_unwaited(const char *base, uint32_t off, uint32_t at) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "{m0}"(at) : "memory");
 }
 
 // The copies this wave issued have landed, and those of every wave once all are
@@ -108,9 +110,8 @@ template <typename T, int D, int NW> struct TileCopy {
   }
   // rows `first` .. of a matrix whose rows are `stride` bytes apart; of the tile's
   // rows only the first nrows (>= 1) exist, the others repeat the last of them
-  __device__ __forceinline__ void issue(char *tile, const char *base, int64_t first, uint32_t stride,
-                                        int nrows) const {
-    const char *src = base + first * (int64_t)stride;
+  __device__ __forceinline__ void issue(uint32_t tile, const char *base, int first, uint32_t stride, int nrows) const {
+    const char *src = base + (int64_t)first * stride;
     if (nrows >= RT::TR) {
 #pragma unroll
       for (int j = 0; j < PW; ++j) copy16_unwaited(src, off[j], tile + (w * PW + j) * 1024);
@@ -127,7 +128,7 @@ template <typename T, int D, int NW> struct TileCopy {
 // follow, those in front of the full ones first.
 struct TileOrder {
   int f0, nfull, h0, nhead, r0, total;
-  // tiles [t0, t1), of which [f0, f1) are seen whole
+  // tiles [t0, t1), of which [fa, fb) are seen whole
   __device__ __forceinline__ TileOrder(int t0, int t1, int fa, int fb) {
     const int f1 = max(t0, min(fb, t1));
     f0 = min(max(fa, t0), f1);
@@ -324,6 +325,7 @@ struct DenseArgs {
   uint64_t magic;                 // 2^40 / G + 1
   float scale, sl2;               // sl2 = scale * log2(e)
   int tiles, splits;
+  bool near;                      // a slice's rows of q and dO lie within 2^32 bytes
 };
 
 // r / G for r < 2^27, G <= 2^12: r * (2^40 / G + 1) errs by less than r / 2^40

@@ -22,11 +22,11 @@ __device__ __forceinline__ float prob(float s, float sl2, float l) {
 // The query side: dQ, and for the key side the rows' log-sum-exps (log2 units;
 // +infinity, weight 0, for rows that see nothing or do not exist) and D.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) dense_dq_kernel(DenseArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dq_kernel(DenseArgs a) {
   using RT = RowTile<T, D>;
-  constexpr int TR = RT::TR;
-  __shared__ __align__(16) char lds0[2 * TR * RT::RB];
-  __shared__ __align__(16) char lds1[2 * TR * RT::RB];
+  constexpr int TR = RT::TR, BYTES = TR * RT::RB;
+  __shared__ __align__(16) char ldsK[2 * BYTES];
+  __shared__ __align__(16) char ldsV[2 * BYTES];
   int s, item;
   dense_block(blockIdx.x, a.B * a.Hkv, a.tiles * a.splits, s, item);
   const int sp = item % a.splits;
@@ -72,11 +72,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) dense_
   const int nt = kend > kbeg ? (kend - kbeg + TR - 1) / TR : 0;
   const int per = (nt + a.splits - 1) / a.splits;
   const int t0 = sp * per, t1 = min(nt, t0 + per);
+  const TileOrder order(t0, t1, (first_key(a, x, b1) - kbeg + TR - 1) / TR, max(0, end_key(a, x, b0) - kbeg) / TR);
+
+  // keys that some row of the wave sees (none: the wave only copies)
   const int wr = tile * DENSE_TQ + 32 * w;
-  const int w0 = wr < a.R ? div_group(a, wr) : x.qlen;
-  const int w1 = min(div_group(a, min(wr + 32, a.R) - 1), x.qlen - 1);
-  const bool busy = w0 <= w1;
-  const int lo0 = first_key(a, x, w0), lo1 = first_key(a, x, w1), hi0 = end_key(a, x, w0), hi1 = end_key(a, x, w1);
+  const int w0 = wr < a.R ? div_group(a, wr) : x.qlen, w1 = min(div_group(a, min(wr + 32, a.R) - 1), x.qlen - 1);
+  const int wlo = first_key(a, x, w0), whi = w0 <= w1 ? end_key(a, x, w1) : 0;
 
   TileAddr<T, D> ad;
   ad.init();
@@ -88,45 +89,42 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) dense_
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dq[i] = splat16(0.f);
 
-  auto issue = [&](int t, char *buf) {
-    const int k0 = kbeg + t * TR;
-    ck.issue(buf, kb, k0, a.k.n, x.klen - k0);
-    cv.issue(buf + TR * RT::RB, vb, k0, a.v.n, x.klen - k0);
+  const uint32_t atK = lds_at(ldsK), atV = lds_at(ldsV);
+  auto issue = [&](int p) {
+    const int k0 = kbeg + order.at(p) * TR;
+    ck.issue(atK + (p & 1) * BYTES, kb, k0, a.k.n, x.klen - k0);
+    cv.issue(atV + (p & 1) * BYTES, vb, k0, a.v.n, x.klen - k0);
   };
-  auto step = [&](const char *buf, int h, int kh, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
-    f32x16 p = tile_rows<T, D>(buf, ad, h, q, splat16(0.f));
-    const f32x16 dp = tile_rows<T, D>(buf + TR * RT::RB, ad, h, dO, splat16(-Dr));
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int j = kh + acc_row(i, g);
-      const float y = prob(p[i], a.sl2, lse2) * dp[i];
-      p[i] = !MASKED || (j >= lo && j < hi) ? y : 0.f;
-    }
-    tile_cols<D>(dq, buf, ad, h, ColsOperand<T>(p));
-  };
-  auto compute = [&](int t, const char *buf) {
-    const int k0 = kbeg + t * TR;
-    if (!busy) return;
-#pragma unroll
-    for (int h = 0; h < TR / 32; ++h) {
-      const int kh = k0 + 32 * h;
-      if (kh >= hi1 || kh + 32 <= lo0) continue;
-      if (kh >= lo1 && kh + 32 <= hi0)
-        step(buf, h, kh, std::false_type{});
-      else
-        step(buf, h, kh, std::true_type{});
-    }
-  };
-  if (t0 < t1) issue(t0, lds0);
-  for (int t = t0; t < t1; t += 2) {
+  auto next = [&](int p) {
     tile_barrier();
-    if (t + 1 < t1) issue(t + 1, lds1);
-    compute(t, lds0);
-    if (t + 1 >= t1) break;
-    tile_barrier();
-    if (t + 2 < t1) issue(t + 2, lds0);
-    compute(t + 1, lds1);
+    if (p + 1 < order.total) issue(p + 1);
+  };
+  auto tiles = [&](int p, int end, auto masked) {
+    for (; p < end; ++p) {
+      next(p);
+      const int k0 = kbeg + order.at(p) * TR;
+      const char *Kt = ldsK + (p & 1) * BYTES, *Vt = ldsV + (p & 1) * BYTES;
+#pragma unroll (D == 64 ? 2 : 1)
+      for (int h = 0; h < TR / 32; ++h) {
+        if (decltype(masked)::value && (k0 + 32 * h >= whi || k0 + 32 * h + 32 <= wlo)) continue;
+        f32x16 z = tile_rows<T, D>(Kt, ad, h, q, splat16(0.f));
+        const f32x16 dp = tile_rows<T, D>(Vt, ad, h, dO, splat16(-Dr));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = k0 + 32 * h + acc_row(i, g);
+          const float y = prob(z[i], a.sl2, lse2) * dp[i];
+          z[i] = !decltype(masked)::value || (j >= lo && j < hi) ? y : 0.f;
+        }
+        tile_cols<D>(dq, Kt, ad, h, ColsOperand<T>(z));
+      }
+    }
+  };
+  if (order.total > 0) issue(0);
+  if (w0 <= w1) {
+    tiles(0, order.nfull, std::false_type{});
+    tiles(order.nfull, order.total, std::true_type{});
+  } else {
+    for (int p = 0; p < order.total; ++p) next(p);
   }
   if (a.splits == 1)
     store_column<D>((T *)(a.dq.p + x.b * a.dq.b + head * a.dq.h + (int64_t)tok * a.dq.n), dq, a.scale, exists);
@@ -136,13 +134,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) dense_
 
 // The key side: dK and dV of 32 keys per wave, over the rows that see them.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) dense_dkv_kernel(DenseArgs a, int ktiles, int ksplits) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dkv_kernel(DenseArgs a, int ktiles, int ksplits) {
   using RT = RowTile<T, D>;
   constexpr int TR = RT::TR;
-  // queries, their gradients, their log-sum-exps and D
-  constexpr int BYTES = 2 * TR * RT::RB + 2 * 256;
-  __shared__ __align__(16) char lds0[BYTES];
-  __shared__ __align__(16) char lds1[BYTES];
+  constexpr int BYTES = TR * RT::RB;
+  __shared__ __align__(16) char ldsQ[2 * BYTES];
+  __shared__ __align__(16) char ldsG[2 * BYTES];  // the queries' gradients
+  __shared__ __align__(16) char ldsL[2 * 512];    // their log-sum-exps (64) and D (64)
   int s, item;
   dense_block(blockIdx.x, a.B * a.Hkv, ktiles * ksplits, s, item);
   const int sp = item % ksplits, kt = item / ksplits;  // causal: the first keys are seen most
@@ -162,14 +160,17 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) dense_
   auto end_row = [&](int j) { return max(0, min(x.qlen, j - x.off + a.left + 1)) * a.G; };
   const int lo = first_row(key), hi = end_row(key);
   const int k0 = kt * DENSE_KB, k1 = min(k0 + DENSE_KB, x.klen);
+  // rows that see some key of the wave (none: the wave only copies)
   const int wk0 = k0 + 32 * w, wk1 = min(wk0 + 32, x.klen) - 1;
-  const bool busy = wk0 <= wk1;
-  const int lo0 = first_row(wk0), lo1 = first_row(wk1), hi0 = end_row(wk0), hi1 = end_row(wk1);
+  const int wlo = first_row(wk0), whi = wk0 <= wk1 ? end_row(wk1) : 0;
   // whole tiles, counted from a multiple of TR
   const int rbeg = k0 < k1 ? first_row(k0) / TR * TR : 0, rend = k0 < k1 ? end_row(k1 - 1) : 0;
   const int nt = rend > rbeg ? (rend - rbeg + TR - 1) / TR : 0;
   const int per = (nt + ksplits - 1) / ksplits;
   const int t0 = sp * per, t1 = min(nt, t0 + per);
+  // tiles whose rows all see the block's keys (rows past the last have no weight)
+  const TileOrder order(t0, t1, (first_row(k1 - 1) - rbeg + TR - 1) / TR,
+                        end_row(k0) >= Rv ? nt : max(0, end_row(k0) - rbeg) / TR);
 
   TileAddr<T, D> ad;
   ad.init();
@@ -180,22 +181,29 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) dense_
   const char *db = a.dO.p + x.b * a.dO.b + (int64_t)x.hk * a.G * a.dO.h;
   const float *rl = a.row_lse + (int64_t)s * a.tiles * DENSE_TQ, *rd = a.row_D + (int64_t)s * a.tiles * DENSE_TQ;
 
-  auto issue = [&](int t, char *buf) {
-    const int r0 = rbeg + t * TR;
+  const uint32_t atQ = lds_at(ldsQ), atG = lds_at(ldsG), atL = lds_at(ldsL);
+  auto issue = [&](int p) {
+    const int r0 = rbeg + order.at(p) * TR;
+    const uint32_t qt = atQ + (p & 1) * BYTES, gt = atG + (p & 1) * BYTES, lt = atL + (p & 1) * 512;
     if (a.G == 1) {
-      cq.issue(buf, qb, r0, a.q.n, Rv - r0);
-      cd.issue(buf + TR * RT::RB, db, r0, a.dO.n, Rv - r0);
+      cq.issue(qt, qb, r0, a.q.n, Rv - r0);
+      cd.issue(gt, db, r0, a.dO.n, Rv - r0);
     } else {
 #pragma unroll
       for (int j = 0; j < cq.PW; ++j) {
         const int r = min(r0 + (int)cq.row[j], Rv - 1), tk = div_group(a, r), h = r - tk * a.G;
-        const int64_t oq = h * a.q.h + (int64_t)tk * a.q.n, od = h * a.dO.h + (int64_t)tk * a.dO.n;
-        copy16(qb + oq + cq.chunk[j], buf + (w * cq.PW + j) * 1024);
-        copy16(db + od + cq.chunk[j], buf + TR * RT::RB + (w * cq.PW + j) * 1024);
+        const int at = (w * cq.PW + j) * 1024;
+        if (a.near) {
+          copy16_unwaited(qb, (uint32_t)h * (uint32_t)a.q.h + (uint32_t)tk * a.q.n + cq.chunk[j], qt + at);
+          copy16_unwaited(db, (uint32_t)h * (uint32_t)a.dO.h + (uint32_t)tk * a.dO.n + cq.chunk[j], gt + at);
+        } else {
+          copy16_unwaited(qb + h * a.q.h + (int64_t)tk * a.q.n + cq.chunk[j], qt + at);
+          copy16_unwaited(db + h * a.dO.h + (int64_t)tk * a.dO.n + cq.chunk[j], gt + at);
+        }
       }
     }
-    if (w == 0) copy4(rl + r0 + lane, buf + 2 * TR * RT::RB);
-    if (w == 1) copy4(rd + r0 + lane, buf + 2 * TR * RT::RB + 256);
+    if (w == 0) copy4_unwaited((const char *)(rl + r0), 4 * lane, lt);
+    if (w == 1) copy4_unwaited((const char *)(rd + r0), 4 * lane, lt + 256);
   };
 
   f32x16 dk[D / 32], dv[D / 32];
@@ -204,57 +212,53 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) dense_
     dk[i] = splat16(0.f);
     dv[i] = splat16(0.f);
   }
-  auto step = [&](const char *buf, int h, int rh, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
-    const float *ls = (const float *)(buf + 2 * TR * RT::RB) + 32 * h + 4 * g, *ds = ls + 64;
-    f32x16 p = tile_rows<T, D>(buf, ad, h, kf, splat16(0.f));
-    f32x16 dp;
+  auto next = [&](int p) {
+    tile_barrier();
+    if (p + 1 < order.total) issue(p + 1);
+  };
+  auto tiles = [&](int p, int end, auto masked) {
+    for (; p < end; ++p) {
+      next(p);
+      const int r0 = rbeg + order.at(p) * TR;
+      const char *qt = ldsQ + (p & 1) * BYTES, *gt = ldsG + (p & 1) * BYTES;
+#pragma unroll (D == 64 ? 2 : 1)
+      for (int h = 0; h < TR / 32; ++h) {
+        if (decltype(masked)::value && (r0 + 32 * h >= whi || r0 + 32 * h + 32 <= wlo)) continue;
+        const float *ls = (const float *)(ldsL + (p & 1) * 512) + 32 * h + 4 * g, *ds = ls + 64;
+        f32x16 z = tile_rows<T, D>(qt, ad, h, kf, splat16(0.f));
+        f32x16 dp;
 #pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {
-      const float4 y = *reinterpret_cast<const float4 *>(ds + 8 * q4);
-      dp[4 * q4] = -y.x;
-      dp[4 * q4 + 1] = -y.y;
-      dp[4 * q4 + 2] = -y.z;
-      dp[4 * q4 + 3] = -y.w;
-    }
-    dp = tile_rows<T, D>(buf + TR * RT::RB, ad, h, vf, dp);
+        for (int c = 0; c < 4; ++c) {
+          const float4 y = *reinterpret_cast<const float4 *>(ds + 8 * c);
+          dp[4 * c] = -y.x;
+          dp[4 * c + 1] = -y.y;
+          dp[4 * c + 2] = -y.z;
+          dp[4 * c + 3] = -y.w;
+        }
+        dp = tile_rows<T, D>(gt, ad, h, vf, dp);
 #pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {
-      const float4 y = *reinterpret_cast<const float4 *>(ls + 8 * q4);
-      const float l[4] = {y.x, y.y, y.z, y.w};
+        for (int c = 0; c < 4; ++c) {
+          const float4 y = *reinterpret_cast<const float4 *>(ls + 8 * c);
+          const float l[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = 4 * q4 + r, at = rh + acc_row(i, g);
-        const float e = prob(p[i], a.sl2, l[r]);
-        p[i] = !MASKED || (at >= lo && at < hi) ? e : 0.f;
-        dp[i] *= p[i];
+          for (int r = 0; r < 4; ++r) {
+            const int i = 4 * c + r, at = r0 + 32 * h + acc_row(i, g);
+            const float e = prob(z[i], a.sl2, l[r]);
+            z[i] = !decltype(masked)::value || (at >= lo && at < hi) ? e : 0.f;
+            dp[i] *= z[i];
+          }
+        }
+        tile_cols<D>(dv, gt, ad, h, ColsOperand<T>(z));
+        tile_cols<D>(dk, qt, ad, h, ColsOperand<T>(dp));
       }
     }
-    tile_cols<D>(dv, buf + TR * RT::RB, ad, h, ColsOperand<T>(p));
-    tile_cols<D>(dk, buf, ad, h, ColsOperand<T>(dp));
   };
-  auto compute = [&](int t, const char *buf) {
-    const int r0 = rbeg + t * TR;
-    if (!busy) return;
-#pragma unroll
-    for (int h = 0; h < TR / 32; ++h) {
-      const int rh = r0 + 32 * h;
-      if (rh >= hi1 || rh + 32 <= lo0) continue;
-      if (rh >= lo1 && rh + 32 <= hi0)
-        step(buf, h, rh, std::false_type{});
-      else
-        step(buf, h, rh, std::true_type{});
-    }
-  };
-  if (t0 < t1) issue(t0, lds0);
-  for (int t = t0; t < t1; t += 2) {
-    tile_barrier();
-    if (t + 1 < t1) issue(t + 1, lds1);
-    compute(t, lds0);
-    if (t + 1 >= t1) break;
-    tile_barrier();
-    if (t + 2 < t1) issue(t + 2, lds0);
-    compute(t + 1, lds1);
+  if (order.total > 0) issue(0);
+  if (wk0 <= wk1) {
+    tiles(0, order.nfull, std::false_type{});
+    tiles(order.nfull, order.total, std::true_type{});
+  } else {
+    for (int p = 0; p < order.total; ++p) next(p);
   }
   if (!valid) {
 #pragma unroll

@@ -54,15 +54,19 @@ template <int D> __device__ __forceinline__ void dense_reference(DenseState<D> &
   }
 }
 
-// s becomes the weights exp2(s sl2 - m), which are added up.
-template <int D> __device__ __forceinline__ void dense_weights(DenseState<D> &st, f32x16 &s, float sl2) {
-  float l[2] = {0.f, 0.f};
+// The weights exp2(s sl2 - m) as they multiply the values; their sum takes them
+// before that rounding (the rounded ones would put the log-sum-exp off by up to
+// 2^-9 over the root of the number of keys).
+template <typename T, int D>
+__device__ __forceinline__ ColsOperand<T> dense_weights(DenseState<D> &st, f32x16 s, float sl2) {
+  float l[2] = {st.l, 0.f};
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], sl2, st.nm));
     l[i & 1] += s[i];
   }
-  st.l += l[0] + l[1];
+  st.l = l[0] + l[1];
+  return ColsOperand<T>(s);
 }
 
 // A column's result (weight sum l, reference m in log2 units) to o and lse, or to
@@ -121,13 +125,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(
   ck.init(a.k.n);
   cv.init(a.v.n);
   const char *kb = a.k.p + x.b * a.k.b + x.hk * a.k.h, *vb = a.v.p + x.b * a.v.b + x.hk * a.v.h;
+  const uint32_t atK = lds_at(ldsK), atV = lds_at(ldsV);
   auto issue_k = [&](int p) {
     const int k0 = kbeg + order.at(p) * TR;
-    ck.issue(ldsK + (p & 1) * BYTES, kb, k0, a.k.n, x.klen - k0);
+    ck.issue(atK + (p & 1) * BYTES, kb, k0, a.k.n, x.klen - k0);
   };
   auto issue_v = [&](int p) {
     const int k0 = kbeg + order.at(p) * TR;
-    cv.issue(ldsV + (p & 1) * BYTES, vb, k0, a.v.n, x.klen - k0);
+    cv.issue(atV + (p & 1) * BYTES, vb, k0, a.v.n, x.klen - k0);
   };
   if (order.total > 0) issue_k(0);
 
@@ -138,25 +143,38 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(
   uint4 q[RT::NS];
   load_column<T, D>(q, a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
   const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
+  // keys that some row of the wave sees (none: the wave only copies)
+  const int wr = tile * DENSE_TQ + 32 * w;
+  const int w0 = wr < a.R ? div_group(a, wr) : x.qlen, w1 = min(div_group(a, min(wr + 32, a.R) - 1), x.qlen - 1);
+  const int wlo = first_key(a, x, w0), whi = w0 <= w1 ? end_key(a, x, w1) : 0;
   DenseState<D> st;
   st.init();
 
   f32x16 sc[HT];
   auto scores = [&](int p, int h) { return tile_rows<T, D>(ldsK + (p & 1) * BYTES, ad, h, q, splat16(0.f)); };
+  auto next = [&](int p) {
+    tile_barrier();
+    if (p + 2 < order.total) issue_k(p + 2);
+    if (p + 1 < order.total) issue_v(p + 1);
+  };
   auto tiles = [&](int p, int end, auto masked) {
     for (; p < end; ++p) {
-      tile_barrier();
-      if (p + 2 < order.total) issue_k(p + 2);
-      if (p + 1 < order.total) issue_v(p + 1);
+      next(p);
       const int k0 = kbeg + order.at(p) * TR;
 #pragma unroll
       for (int h = 0; h < HT; ++h) {
         f32x16 now = sc[h];
-        if (decltype(masked)::value) dense_mask(now, lo - k0 - 32 * h, hi - k0 - 32 * h);
+        const int kh = k0 + 32 * h;
+        if (decltype(masked)::value) {
+          if (kh >= whi || kh + 32 <= wlo) {
+            sc[h] = scores(p + 1, h);
+            continue;
+          }
+          dense_mask(now, lo - kh, hi - kh);
+        }
         dense_reference<D>(st, now, a.sl2);
         sc[h] = scores(p + 1, h);  // (past the last tile: unused)
-        dense_weights<D>(st, now, a.sl2);
-        tile_cols<D>(st.o, ldsV + (p & 1) * BYTES, ad, h, ColsOperand<T>(now));
+        tile_cols<D>(st.o, ldsV + (p & 1) * BYTES, ad, h, dense_weights<T, D>(st, now, a.sl2));
       }
     }
   };
@@ -164,20 +182,24 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(
     tile_barrier();
     if (order.total > 1) issue_k(1);
     issue_v(0);
+    if (w0 <= w1) {
 #pragma unroll
-    for (int h = 0; h < HT; ++h) sc[h] = scores(0, h);
-    tiles(0, order.nfull, std::false_type{});
-    tiles(order.nfull, order.total, std::true_type{});
+      for (int h = 0; h < HT; ++h) sc[h] = scores(0, h);
+      tiles(0, order.nfull, std::false_type{});
+      tiles(order.nfull, order.total, std::true_type{});
+    } else {
+      for (int p = 0; p < order.total; ++p) next(p);
+    }
   }
   dense_write<T, D>(a, x, s, sp, row, tok, head, exists, valid, column_sum(st.l), -st.nm, st.o);
 }
 
-// At most 32 rows per slice (single tokens): the four waves of a workgroup share
-// the rows and take the block's 32-key tiles in turn, each with tiles of its own
-// in LDS and no barrier, so that every wave streams keys. Bound by the bytes of K
-// and V: a wave refills its K tile while the values multiply and its V tile while
-// the next scores form. The waves' results are joined at the end by their
-// reference maxima.
+// Few rows (single tokens, small problems): the four waves of a workgroup share 32
+// rows and take the block's 32-key tiles in turn, each with tiles of its own in LDS
+// and no barrier, so that every wave streams keys. Bound by the bytes of K and V,
+// or in small problems by one wave's chain over its quarter of the keys: a wave
+// refills its K tile while the values multiply and its V tile while the next scores
+// form. The waves' results are joined at the end by their reference maxima.
 template <typename T, int D> struct FewTile {
   using RT = RowTile<T, D>;
   static constexpr int NW = 4, BYTES = 32 * RT::RB, NI = 32 / RT::RPI;  // copies per tile and wave
@@ -185,10 +207,10 @@ template <typename T, int D> struct FewTile {
 
 // The wave's next tile: rows past the last repeat it.
 template <typename T, int D>
-__device__ __forceinline__ void few_copy(char *tile, const char *base, int64_t first, uint32_t stride, int nrows) {
+__device__ __forceinline__ void few_copy(uint32_t tile, const char *base, int first, uint32_t stride, int nrows) {
   using RT = RowTile<T, D>;
   const int lane = threadIdx.x & 63;
-  const char *src = base + first * (int64_t)stride;
+  const char *src = base + (int64_t)first * stride;
 #pragma unroll
   for (int j = 0; j < FewTile<T, D>::NI; ++j) {
     const int r = j * RT::RPI + lane / RT::CPR;
@@ -203,27 +225,31 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) ==
   __shared__ __align__(16) char ldsK[FT::NW * FT::BYTES];
   __shared__ __align__(16) char ldsV[FT::NW * FT::BYTES];
   __shared__ float join_m[FT::NW][32], join_l[FT::NW][32];
-  int s, sp;
-  dense_block(blockIdx.x, a.B * a.Hkv, a.splits, s, sp);
+  int s, item;
+  dense_block(blockIdx.x, a.B * a.Hkv, a.tiles * a.splits, s, item);
+  const int sp = item % a.splits;
+  const int tile = a.tiles - 1 - item / a.splits;  // causal: the longest first
   const DenseSlice x = dense_slice(a, s);
   const int lane = threadIdx.x & 63, n = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 
-  const int tok = div_group(a, n), head = x.hk * a.G + n - tok * a.G;
-  const bool exists = n < a.R, valid = exists && tok < x.qlen;
-  const int last = min(a.N, x.qlen) - 1;  // the last query (-1: none)
-  const int kbeg = first_key(a, x, 0), kend = last >= 0 ? end_key(a, x, last) : 0;
+  const int row = 32 * tile + n;
+  const int tok = div_group(a, row), head = x.hk * a.G + row - tok * a.G;
+  const bool exists = row < a.R, valid = exists && tok < x.qlen;
+  const int b0 = div_group(a, 32 * tile), b1 = min(div_group(a, min(32 * tile + 32, a.R) - 1), x.qlen - 1);
+  const int kbeg = first_key(a, x, b0), kend = b0 <= b1 ? end_key(a, x, b1) : 0;
   const int nt = kend > kbeg ? (kend - kbeg + 31) / 32 : 0;
   const int per = (nt + a.splits - 1) / a.splits;
   const int t1 = min(nt, (sp + 1) * per);
   const char *kb = a.k.p + x.b * a.k.b + x.hk * a.k.h, *vb = a.v.p + x.b * a.v.b + x.hk * a.v.h;
-  char *Kt = ldsK + w * FT::BYTES, *Vt = ldsV + w * FT::BYTES;
+  const char *Kt = ldsK + w * FT::BYTES, *Vt = ldsV + w * FT::BYTES;
+  const uint32_t atK = lds_at(ldsK) + w * FT::BYTES, atV = lds_at(ldsV) + w * FT::BYTES;
 
   uint4 q[RT::NS];
   load_column<T, D>(q, a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
   const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
   // keys in [lo1, hi0) are seen by every query
-  const int lo1 = first_key(a, x, last), hi0 = end_key(a, x, 0);
+  const int lo1 = first_key(a, x, b1), hi0 = end_key(a, x, b0);
   TileAddr<T, D> ad;
   ad.init();
   DenseState<D> st;
@@ -231,8 +257,8 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) ==
   int t = sp * per + w;
   if (t < t1) {
     const int k0 = kbeg + 32 * t;
-    few_copy<T, D>(Kt, kb, k0, a.k.n, x.klen - k0);
-    few_copy<T, D>(Vt, vb, k0, a.v.n, x.klen - k0);
+    few_copy<T, D>(atK, kb, k0, a.k.n, x.klen - k0);
+    few_copy<T, D>(atV, vb, k0, a.v.n, x.klen - k0);
   }
   wait_copies<0>();  // (the queries too: no wait for them inside the loop)
   for (; t < t1; t += FT::NW) {
@@ -241,17 +267,17 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) ==
     wait_copies<FT::NI>();  // K is here, V may be in flight
     f32x16 sc = tile_rows<T, D>(Kt, ad, 0, q, splat16(0.f));
     wait_lds();  // and has been read
-    if (more) few_copy<T, D>(Kt, kb, k1, a.k.n, x.klen - k1);
+    if (more) few_copy<T, D>(atK, kb, k1, a.k.n, x.klen - k1);
     if (!(k0 >= lo1 && k0 + 32 <= hi0)) dense_mask(sc, lo - k0, hi - k0);
     dense_reference<D>(st, sc, a.sl2);
-    dense_weights<D>(st, sc, a.sl2);
+    const ColsOperand<T> P = dense_weights<T, D>(st, sc, a.sl2);
     if (more)
       wait_copies<FT::NI>();  // V is here, the next K may be in flight
     else
       wait_copies<0>();
-    tile_cols<D>(st.o, Vt, ad, 0, ColsOperand<T>(sc));
+    tile_cols<D>(st.o, Vt, ad, 0, P);
     wait_lds();
-    if (more) few_copy<T, D>(Vt, vb, k1, a.v.n, x.klen - k1);
+    if (more) few_copy<T, D>(atV, vb, k1, a.v.n, x.klen - k1);
   }
 
   // every wave's sums relative to the common maximum, added in pairs: waves 0 and
@@ -279,7 +305,7 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) ==
   __syncthreads();
   if (w >= 1) return;
   each([&](float o, int e) { return o + jv[e * 64]; });
-  dense_write<T, D>(a, x, s, sp, n, tok, head, exists, valid, (join_l[0][n] + join_l[2][n]) + (join_l[1][n] + join_l[3][n]),
+  dense_write<T, D>(a, x, s, sp, row, tok, head, exists, valid, (join_l[0][n] + join_l[2][n]) + (join_l[1][n] + join_l[3][n]),
                     m, st.o);
 }
 
@@ -344,13 +370,15 @@ DenseArgs dense_args(const mita_dense_cfg_t &c) {
   a.magic = ((uint64_t)1 << 40) / (uint64_t)a.G + 1;
   a.scale = eff_scale(c);
   a.sl2 = a.scale * LOG2E;
+  a.near = true;
+  for (const DenseMat *m : {&a.q, &a.dO})
+    a.near = a.near && (a.G - 1) * m->h + (int64_t)a.N * m->n + 1024 < ((int64_t)1 << 32);
   return a;
 }
 
 namespace {
-template <typename T, int D> hipError_t forward_t(const DenseArgs &a, hipStream_t st) {
+template <typename T, int D> hipError_t forward_t(const DenseArgs &a, bool few, hipStream_t st) {
   const dim3 grid((unsigned)(a.B * a.Hkv) * a.tiles * a.splits);
-  const bool few = a.R <= DENSE_FEW;
   if (few)
     dense_few_kernel<T, D><<<grid, 256, 0, st>>>(a);
   else
@@ -382,8 +410,8 @@ hipError_t launch_dense_forward(const mita_dense_cfg_t &c, const void *q, const 
     a.part_o = (float *)((char *)ws + L.part_o);
     a.part_lse = (float *)((char *)ws + L.part_lse);
   }
-  if (c.dtype == MITA_F32) return c.d == 64 ? forward_t<float, 64>(a, st) : forward_t<float, 128>(a, st);
-  return c.d == 64 ? forward_t<bf16_t, 64>(a, st) : forward_t<bf16_t, 128>(a, st);
+  if (c.dtype == MITA_F32) return c.d == 64 ? forward_t<float, 64>(a, p.few, st) : forward_t<float, 128>(a, p.few, st);
+  return c.d == 64 ? forward_t<bf16_t, 64>(a, p.few, st) : forward_t<bf16_t, 128>(a, p.few, st);
 }
 
 }  // namespace mita

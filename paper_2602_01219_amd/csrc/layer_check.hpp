@@ -13,7 +13,7 @@
 namespace mita {
 
 constexpr int DENSE_TQ = 128;  // query rows of a dense attention workgroup (32 per wave)
-constexpr int DENSE_FEW = 32;   // rows per slice up to which a workgroup's waves share them
+constexpr int DENSE_FEW = 32;   // ... and of one whose waves share the rows
 constexpr int DENSE_KB = 128;  // keys of a key-side backward workgroup
 constexpr int CUS = 256;       // compute units of the MI355X
 constexpr int DENSE_MAX_SPLITS = 64;
@@ -186,11 +186,12 @@ inline int window(int w, const mita_dense_cfg_t &c) {
   return w < 0 || w > none ? none : w;
 }
 
-// Launch plan of the forward. A workgroup takes DENSE_TQ rows of a slice. With
-// fewer than two workgroups per CU the keys of each are split: enough splits
-// for two per CU, at least 512 keys each; the splits' results are joined by
-// their log-sum-exps.
+// Launch plan of the forward. A workgroup takes DENSE_TQ rows of a slice, or, where
+// those leave CUs without work, DENSE_FEW rows whose keys its waves share. While
+// workgroups are few (two fit a CU) the keys of each are split, at least 512 keys
+// each; the splits' results are joined by their log-sum-exps.
 struct DensePlan {
+  bool few;    // DENSE_FEW rows per workgroup
   int tiles;   // row tiles per slice
   int splits;  // key splits per row tile
 };
@@ -200,21 +201,31 @@ inline int keys_seen(const mita_dense_cfg_t &c) {  // most keys one row tile rea
   if (c.left >= 0 && c.right >= 0) m = std::min<int64_t>(m, span + c.left + (int64_t)c.right);
   return (int)m;
 }
-inline int splits_for(int64_t blocks, int64_t len, int64_t least) {
-  const int64_t want = (2 * CUS + blocks - 1) / blocks;
+// `uneven`: the window gives workgroups different lengths, which even out over two
+// rounds of them (16 heads of 4 key heads, 8192 tokens, causal, d = 128, backward:
+// 1718 us with one round).
+inline int splits_for(int64_t blocks, int64_t len, int64_t least, bool uneven) {
+  // (rounded down: 960 workgroups of a causal forward, 5 sequences of 2039 tokens,
+  // d = 128, take 62 us whole and 103 split in two, by the partial results)
+  const int64_t want = (uneven ? 4 : 2) * CUS / blocks;
   return (int)std::max<int64_t>(1, std::min<int64_t>({want, len / least, (int64_t)DENSE_MAX_SPLITS}));
 }
+inline bool uneven(const mita_dense_cfg_t &c) { return (c.left >= 0) != (c.right >= 0); }
 inline DensePlan dense_plan(const mita_dense_cfg_t &c) {
   DensePlan p;
   p.tiles = (int)((dense_rows(c) + DENSE_TQ - 1) / DENSE_TQ);
-  p.splits = splits_for(slices(c) * p.tiles, keys_seen(c), 512);
-  if (dense_rows(c) <= DENSE_FEW) {
-    // a few rows stream keys: just over two workgroups per CU (192 slices of up to
-    // 16384 keys, d = 128: 217 us; one per CU 234, four 229, eight 242, as every
-    // workgroup starts with nothing in flight), 256 keys each at least
-    const int64_t want = (2 * CUS) / slices(c) + 1;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, keys_seen(c) / 256, (int64_t)DENSE_MAX_SPLITS}));
+  p.few = dense_rows(c) <= DENSE_FEW || slices(c) * p.tiles < CUS;
+  if (!p.few) {
+    p.splits = splits_for(slices(c) * p.tiles, keys_seen(c), 512, uneven(c));
+    return p;
   }
+  p.tiles = (int)((dense_rows(c) + DENSE_FEW - 1) / DENSE_FEW);
+  // just over two workgroups per CU (192 slices of up to 16384 keys, d = 128: 217 us;
+  // one per CU 234, four 229, eight 242, as every workgroup starts with nothing in
+  // flight), 256 keys each at least (1024 of more rows, whose join takes 4 us)
+  const int64_t blocks = slices(c) * p.tiles, want = (2 * CUS) / blocks + (dense_rows(c) <= DENSE_FEW ? 1 : 0);
+  const int64_t least = dense_rows(c) <= DENSE_FEW ? 256 : 1024;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, keys_seen(c) / least, (int64_t)DENSE_MAX_SPLITS}));
   return p;
 }
 
@@ -226,12 +237,12 @@ struct DenseBwdPlan {
 inline DenseBwdPlan dense_bwd_plan(const mita_dense_cfg_t &c) {
   DenseBwdPlan p;
   p.qtiles = (int)((dense_rows(c) + DENSE_TQ - 1) / DENSE_TQ);
-  p.qsplits = splits_for(slices(c) * p.qtiles, keys_seen(c), 512);
+  p.qsplits = splits_for(slices(c) * p.qtiles, keys_seen(c), 512, uneven(c));
   p.ktiles = (c.N_k + DENSE_KB - 1) / DENSE_KB;
   int64_t rows = dense_rows(c);
   if (c.left >= 0 && c.right >= 0)
     rows = std::min<int64_t>(rows, (DENSE_KB + (int64_t)c.left + c.right + 1) * group(c));
-  p.ksplits = splits_for(slices(c) * p.ktiles, rows, 512);
+  p.ksplits = splits_for(slices(c) * p.ktiles, rows, 512, uneven(c));
   return p;
 }
 

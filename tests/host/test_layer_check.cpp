@@ -119,7 +119,7 @@ int main() {
             x.right = w < 0 ? -1 : 0;
             const DensePlan p = dense_plan(x);
             const DenseBwdPlan q = dense_bwd_plan(x);
-            CHECK(p.tiles >= 1 && (int64_t)p.tiles * DENSE_TQ >= dense_rows(x));
+            CHECK(p.tiles >= 1 && (int64_t)p.tiles * (p.few ? DENSE_FEW : DENSE_TQ) >= dense_rows(x));
             CHECK(p.splits >= 1 && p.splits <= DENSE_MAX_SPLITS);
             CHECK(q.qsplits >= 1 && q.ksplits >= 1 && q.ktiles * DENSE_KB >= Nk);
             if (p.splits > 1) CHECK(slices(x) * p.tiles < 2 * CUS);
