@@ -88,37 +88,42 @@ __device__ __forceinline__ void wait_lds() {
 }
 
 // A tile's copy into LDS by DMA (global_load_lds_dwordx4), NW waves: lane l of
-// copy `ins` fills slot l % CPR of row ins * RPI + l / CPR.
+// copy `ins` fills slot l % CPR of row ins * RPI + l / CPR. swz is linear over the
+// bits of the row, and a wave's copies j differ in bits of their own, so copy j's
+// chunk is that of its first XOR swz(j RPI).
 template <typename T, int D, int NW> struct TileCopy {
   using RT = RowTile<T, D>;
   static constexpr int PW = RT::TR / RT::RPI / NW;  // copies per wave
   static_assert(PW >= 1 && RT::TR % (RT::RPI * NW) == 0, "whole copies per wave");
-  int w;               // the wave, as a scalar
-  uint32_t row[PW];    // the lane's row of each copy
-  uint32_t chunk[PW];  // byte offset of its chunk in the row
-  uint32_t off[PW];    // row * stride + chunk, for whole tiles
-  __device__ __forceinline__ void init(uint32_t stride) {
+  int w;           // the wave, as a scalar
+  uint32_t row0;   // the lane's row of the wave's first copy
+  uint32_t chunk0; // byte offset of its chunk in the row
+  __device__ __forceinline__ void init() {
     w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int j = 0; j < PW; ++j) {
-      const int r = (w * PW + j) * RT::RPI + lane / RT::CPR;
-      row[j] = (uint32_t)r;
-      chunk[j] = (uint32_t)(((lane % RT::CPR) ^ RT::swz(r)) << 4);
-      off[j] = row[j] * stride + chunk[j];
-    }
+    const int lane = threadIdx.x & 63, r = w * PW * RT::RPI + lane / RT::CPR;
+    row0 = (uint32_t)r;
+    chunk0 = (uint32_t)(((lane % RT::CPR) ^ RT::swz(r)) << 4);
   }
-  // rows `first` .. of a matrix whose rows are `stride` bytes apart; of the tile's
-  // rows only the first nrows (>= 1) exist, the others repeat the last of them
-  __device__ __forceinline__ void issue(uint32_t tile, const char *base, int first, uint32_t stride, int nrows) const {
+  __device__ __forceinline__ void forget() {  // (see TileAddr)
+    pin(row0);
+    pin(chunk0);
+  }
+  __device__ __forceinline__ uint32_t row(int j) const { return row0 + j * RT::RPI; }
+  __device__ __forceinline__ uint32_t chunk(int j) const { return chunk0 ^ (uint32_t)(RT::swz(j * RT::RPI) << 4); }
+  // rows `first` .. of a matrix whose rows are `stride` bytes apart (off0 = row0
+  // stride); of the tile's rows only the first nrows (>= 1) exist, the others
+  // repeat the last of them
+  __device__ __forceinline__ void issue(uint32_t tile, const char *base, int first, uint32_t stride, uint32_t off0,
+                                        int nrows) const {
     const char *src = base + (int64_t)first * stride;
     if (nrows >= RT::TR) {
 #pragma unroll
-      for (int j = 0; j < PW; ++j) copy16_unwaited(src, off[j], tile + (w * PW + j) * 1024);
+      for (int j = 0; j < PW; ++j)
+        copy16_unwaited(src + (uint64_t)(j * RT::RPI) * stride, off0 + chunk(j), tile + (w * PW + j) * 1024);
     } else {
 #pragma unroll
       for (int j = 0; j < PW; ++j)
-        copy16_unwaited(src, min(row[j], (uint32_t)(nrows - 1)) * stride + chunk[j], tile + (w * PW + j) * 1024);
+        copy16_unwaited(src, min(row(j), (uint32_t)(nrows - 1)) * stride + chunk(j), tile + (w * PW + j) * 1024);
     }
   }
 };
@@ -147,28 +152,30 @@ struct TileOrder {
 // Per-lane LDS addresses of the two products, fixed for every tile.
 template <typename T, int D> struct TileAddr {
   using RT = RowTile<T, D>;
-  uint32_t r0;                                     // `rows`: chunk g of row n; step s is r0 ^ (s << 5)
-  uint32_t c[sizeof(T) == 2 ? 2 * RT::NB : 1];     // `cols`, see tile_cols
+  uint32_t r0;  // `rows`: chunk g of row n; step s is r0 ^ (s << 5)
+  uint32_t c0;  // `cols`: see col
   __device__ __forceinline__ void init() {
     const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
     r0 = (uint32_t)(n * RT::RB + ((g ^ RT::swz(n)) << 4));
     if constexpr (sizeof(T) == 2) {
       // 16-lane groups read 4 x 16 blocks transposed (ds_read_b64_tr_b16: lane
-      // 4 e + p addresses piece p of row e, lane i receives column i): rows
-      // 8 h + 4 g + e, columns 32 db + 16 ((lane >> 4) & 1) + i
-      const int e = (lane & 15) >> 2, p = lane & 3, half = (lane >> 4) & 1;
-#pragma unroll
-      for (int db = 0; db < RT::NB; ++db)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = 8 * h + 4 * g + e;
-          c[2 * db + h] = (uint32_t)(r * RT::RB + (((4 * db + 2 * half + (p >> 1)) ^ RT::swz(r)) << 4) + ((p & 1) << 3));
-          pin(c[2 * db + h]);
-        }
+      // 4 e + p addresses piece p of row e, lane i receives column i)
+      const int e = (lane & 15) >> 2, p = lane & 3, half = (lane >> 4) & 1, r = 4 * g + e;
+      c0 = (uint32_t)(r * RT::RB + (((2 * half + (p >> 1)) ^ RT::swz(r)) << 4) + ((p & 1) << 3));
     } else {
-      // row 8 q + 4 g + r, element n of block db: c ^ (db << 7) ^ swizzle(q, r), + (8 q + r) rows
-      c[0] = (uint32_t)(4 * g * RT::RB + (((n >> 2) ^ (g << 3)) << 4) + ((n & 3) << 2));
+      // row 8 q + 4 g + r, element n of block db: c0 ^ (db << 7) ^ swizzle(q, r), + (8 q + r) rows
+      c0 = (uint32_t)(4 * g * RT::RB + (((n >> 2) ^ (g << 3)) << 4) + ((n & 3) << 2));
     }
+  }
+  // bf16: rows 8 h + 4 g + e of 16, columns 32 db + 16 ((lane >> 4) & 1) + i
+  __device__ __forceinline__ uint32_t col(int db, int h) const {
+    return (c0 ^ (uint32_t)(((4 * db) ^ RT::swz(8 * h)) << 4)) + (uint32_t)(8 * h * RT::RB);
+  }
+  // Addresses that derive from these are formed again where they are used from
+  // here on, instead of being kept in registers.
+  __device__ __forceinline__ void forget() {
+    pin(r0);
+    pin(c0);
   }
 };
 
@@ -226,7 +233,7 @@ __device__ __forceinline__ void tile_cols(f32x16 (&acc)[D / 32], const char *til
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         h[i] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                             (lds_v4i16_t *)(tile + ad.c[2 * db + i] + (32 * kb + 16 * s) * RT::RB)));
+                                             (lds_v4i16_t *)(tile + ad.col(db, i) + (32 * kb + 16 * s) * RT::RB)));
       acc[db] = mma32((bf16_t *)nullptr, make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), P.b[s], acc[db]);
     }
 }
@@ -237,7 +244,7 @@ __device__ __forceinline__ void tile_cols(f32x16 (&acc)[D / 32], const char *til
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int q = i >> 2, r = i & 3;
-    const uint32_t at = ad.c[0] ^ (uint32_t)(((q & 1) << 2 | r) << 4);
+    const uint32_t at = ad.c0 ^ (uint32_t)(((q & 1) << 2 | r) << 4);
 #pragma unroll
     for (int db = 0; db < RT::NB; ++db) {
       const float a =
@@ -356,13 +363,15 @@ __device__ __forceinline__ int end_key(const DenseArgs &a, const DenseSlice &x, 
 
 // Block id -> (slice, work item of the slice). Consecutive ids go to the eight
 // XCDs in turn; a slice's items stay on one XCD, whose L2 then holds the rows
-// they share, except for the last S % 8 slices, whose items go round all XCDs.
-__device__ __forceinline__ void dense_block(int id, int S, int items, int &slice, int &item) {
+// they share, except for the last S % 8 slices, whose items go round all XCDs. The
+// slices come to the XCDs in snake order, which evens out lengths that fall (or
+// rise) over the batch.
+__device__ __forceinline__ void dense_block(int id, int S, int items, int &slice, int &item, bool snake = true) {
   const int whole = S & ~7;
   if (id < whole * items) {
-    const int j = id >> 3;
-    slice = (id & 7) + 8 * (j / items);
-    item = j % items;
+    const int j = id >> 3, round = j / items;
+    slice = 8 * round + (snake && (round & 1) ? 7 - (id & 7) : id & 7);
+    item = j - round * items;
   } else {
     const int j = id - whole * items, rest = S - whole;
     // items outermost: the heavy first items of every slice start first

@@ -22,7 +22,7 @@ __device__ __forceinline__ float prob(float s, float sl2, float l) {
 // The query side: dQ, and for the key side the rows' log-sum-exps (log2 units;
 // +infinity, weight 0, for rows that see nothing or do not exist) and D.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dq_kernel(DenseArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) * D == 128 ? 3 : sizeof(T) * D == 256 ? 2 : 1) dense_dq_kernel(DenseArgs a) {
   using RT = RowTile<T, D>;
   constexpr int TR = RT::TR, BYTES = TR * RT::RB;
   __shared__ __align__(16) char ldsK[2 * BYTES];
@@ -81,9 +81,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dq_kernel(D
 
   TileAddr<T, D> ad;
   ad.init();
-  TileCopy<T, D, 4> ck, cv;
-  ck.init(a.k.n);
-  cv.init(a.v.n);
+  TileCopy<T, D, 4> copy;
+  copy.init();
+  const uint32_t offK = copy.row0 * a.k.n, offV = copy.row0 * a.v.n;
   const char *kb = a.k.p + x.b * a.k.b + x.hk * a.k.h, *vb = a.v.p + x.b * a.v.b + x.hk * a.v.h;
   f32x16 dq[D / 32];
 #pragma unroll
@@ -92,8 +92,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dq_kernel(D
   const uint32_t atK = lds_at(ldsK), atV = lds_at(ldsV);
   auto issue = [&](int p) {
     const int k0 = kbeg + order.at(p) * TR;
-    ck.issue(atK + (p & 1) * BYTES, kb, k0, a.k.n, x.klen - k0);
-    cv.issue(atV + (p & 1) * BYTES, vb, k0, a.v.n, x.klen - k0);
+    copy.issue(atK + (p & 1) * BYTES, kb, k0, a.k.n, offK, x.klen - k0);
+    copy.issue(atV + (p & 1) * BYTES, vb, k0, a.v.n, offV, x.klen - k0);
   };
   auto next = [&](int p) {
     tile_barrier();
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dq_kernel(D
 
 // The key side: dK and dV of 32 keys per wave, over the rows that see them.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dkv_kernel(DenseArgs a, int ktiles, int ksplits) {
+__global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_dkv_kernel(DenseArgs a, int ktiles, int ksplits) {
   using RT = RowTile<T, D>;
   constexpr int TR = RT::TR;
   constexpr int BYTES = TR * RT::RB;
@@ -174,36 +174,37 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dkv_kernel(
 
   TileAddr<T, D> ad;
   ad.init();
-  TileCopy<T, D, 4> cq, cd;
-  cq.init(a.q.n);
-  cd.init(a.dO.n);
+  TileCopy<T, D, 4> copy;
+  copy.init();
   const char *qb = a.q.p + x.b * a.q.b + (int64_t)x.hk * a.G * a.q.h;
   const char *db = a.dO.p + x.b * a.dO.b + (int64_t)x.hk * a.G * a.dO.h;
   const float *rl = a.row_lse + (int64_t)s * a.tiles * DENSE_TQ, *rd = a.row_D + (int64_t)s * a.tiles * DENSE_TQ;
 
   const uint32_t atQ = lds_at(ldsQ), atG = lds_at(ldsG), atL = lds_at(ldsL);
   auto issue = [&](int p) {
+    if (D == 128) copy.forget();
     const int r0 = rbeg + order.at(p) * TR;
     const uint32_t qt = atQ + (p & 1) * BYTES, gt = atG + (p & 1) * BYTES, lt = atL + (p & 1) * 512;
     if (a.G == 1) {
-      cq.issue(qt, qb, r0, a.q.n, Rv - r0);
-      cd.issue(gt, db, r0, a.dO.n, Rv - r0);
+      copy.issue(qt, qb, r0, a.q.n, copy.row0 * a.q.n, Rv - r0);
+      copy.issue(gt, db, r0, a.dO.n, copy.row0 * a.dO.n, Rv - r0);
     } else {
 #pragma unroll
-      for (int j = 0; j < cq.PW; ++j) {
-        const int r = min(r0 + (int)cq.row[j], Rv - 1), tk = div_group(a, r), h = r - tk * a.G;
-        const int at = (w * cq.PW + j) * 1024;
+      for (int j = 0; j < copy.PW; ++j) {
+        const int r = min(r0 + (int)copy.row(j), Rv - 1), tk = div_group(a, r), h = r - tk * a.G;
+        const int at = (w * copy.PW + j) * 1024;
         if (a.near) {
-          copy16_unwaited(qb, (uint32_t)h * (uint32_t)a.q.h + (uint32_t)tk * a.q.n + cq.chunk[j], qt + at);
-          copy16_unwaited(db, (uint32_t)h * (uint32_t)a.dO.h + (uint32_t)tk * a.dO.n + cq.chunk[j], gt + at);
+          copy16_unwaited(qb, (uint32_t)h * (uint32_t)a.q.h + (uint32_t)tk * a.q.n + copy.chunk(j), qt + at);
+          copy16_unwaited(db, (uint32_t)h * (uint32_t)a.dO.h + (uint32_t)tk * a.dO.n + copy.chunk(j), gt + at);
         } else {
-          copy16_unwaited(qb + h * a.q.h + (int64_t)tk * a.q.n + cq.chunk[j], qt + at);
-          copy16_unwaited(db + h * a.dO.h + (int64_t)tk * a.dO.n + cq.chunk[j], gt + at);
+          copy16_unwaited(qb + h * a.q.h + (int64_t)tk * a.q.n + copy.chunk(j), qt + at);
+          copy16_unwaited(db + h * a.dO.h + (int64_t)tk * a.dO.n + copy.chunk(j), gt + at);
         }
       }
     }
-    if (w == 0) copy4_unwaited((const char *)(rl + r0), 4 * lane, lt);
-    if (w == 1) copy4_unwaited((const char *)(rd + r0), 4 * lane, lt + 256);
+    const uint32_t at4 = 4 * lanes_below(~(uint64_t)0);
+    if (w == 0) copy4_unwaited((const char *)(rl + r0), at4, lt);
+    if (w == 1) copy4_unwaited((const char *)(rd + r0), at4, lt + 256);
   };
 
   f32x16 dk[D / 32], dv[D / 32];
@@ -223,6 +224,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_dkv_kernel(
       const char *qt = ldsQ + (p & 1) * BYTES, *gt = ldsG + (p & 1) * BYTES;
 #pragma unroll (D == 64 ? 2 : 1)
       for (int h = 0; h < TR / 32; ++h) {
+        if (D == 128) ad.forget();  // (registers are short)
         if (decltype(masked)::value && (r0 + 32 * h >= whi || r0 + 32 * h + 32 <= wlo)) continue;
         const float *ls = (const float *)(ldsL + (p & 1) * 512) + 32 * h + 4 * g, *ds = ls + 64;
         f32x16 z = tile_rows<T, D>(qt, ad, h, kf, splat16(0.f));

@@ -96,7 +96,7 @@ __device__ __forceinline__ void dense_write(const DenseArgs &a, const DenseSlice
 // forms the scores of the next tile while it weighs the present one, so that its
 // MFMAs have VALU work to run beside, and two waves share a SIMD.
 template <typename T, int D>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(DenseArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_fwd_kernel(DenseArgs a) {
   using RT = RowTile<T, D>;
   constexpr int TR = RT::TR, HT = TR / 32, BYTES = TR * RT::RB;
   __shared__ __align__(16) char ldsK[2 * BYTES];
@@ -121,18 +121,18 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_fwd_kernel(
 
   TileAddr<T, D> ad;
   ad.init();
-  TileCopy<T, D, 4> ck, cv;
-  ck.init(a.k.n);
-  cv.init(a.v.n);
+  TileCopy<T, D, 4> copy;
+  copy.init();
+  const uint32_t offK = copy.row0 * a.k.n, offV = copy.row0 * a.v.n;
   const char *kb = a.k.p + x.b * a.k.b + x.hk * a.k.h, *vb = a.v.p + x.b * a.v.b + x.hk * a.v.h;
   const uint32_t atK = lds_at(ldsK), atV = lds_at(ldsV);
   auto issue_k = [&](int p) {
     const int k0 = kbeg + order.at(p) * TR;
-    ck.issue(atK + (p & 1) * BYTES, kb, k0, a.k.n, x.klen - k0);
+    copy.issue(atK + (p & 1) * BYTES, kb, k0, a.k.n, offK, x.klen - k0);
   };
   auto issue_v = [&](int p) {
     const int k0 = kbeg + order.at(p) * TR;
-    cv.issue(atV + (p & 1) * BYTES, vb, k0, a.v.n, x.klen - k0);
+    copy.issue(atV + (p & 1) * BYTES, vb, k0, a.v.n, offV, x.klen - k0);
   };
   if (order.total > 0) issue_k(0);
 
@@ -219,14 +219,14 @@ __device__ __forceinline__ void few_copy(uint32_t tile, const char *base, int fi
   }
 }
 
-template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) dense_few_kernel(DenseArgs a) {
+template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_few_kernel(DenseArgs a) {
   using RT = RowTile<T, D>;
   using FT = FewTile<T, D>;
   __shared__ __align__(16) char ldsK[FT::NW * FT::BYTES];
   __shared__ __align__(16) char ldsV[FT::NW * FT::BYTES];
   __shared__ float join_m[FT::NW][32], join_l[FT::NW][32];
   int s, item;
-  dense_block(blockIdx.x, a.B * a.Hkv, a.tiles * a.splits, s, item);
+  dense_block(blockIdx.x, a.B * a.Hkv, a.tiles * a.splits, s, item, false);
   const int sp = item % a.splits;
   const int tile = a.tiles - 1 - item / a.splits;  // causal: the longest first
   const DenseSlice x = dense_slice(a, s);
