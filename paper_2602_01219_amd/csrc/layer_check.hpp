@@ -346,39 +346,41 @@ inline int check_norm(const mita_norm_cfg_t *c, std::string *err) {
 
 // Geometry of the norm kernels: `tpr` threads take a row, each `p` pieces of `ve`
 // elements; p == 0: rows too wide for registers, read again in each pass.
-constexpr int NORM_FWD_THREADS = 256, NORM_BWD_THREADS = 512;
+constexpr int NORM_FWD_THREADS = 256, NORM_BWD_THREADS = 512;  // per workgroup, or tpr if that is more
 struct NormPlan {
   int ve, tpr, p;
 };
-inline NormPlan norm_plan(const mita_norm_cfg_t &c, bool vec) {
-  const int ve = vec ? 16 / (int)elem_bytes(c) : 1;
-  const int n = (c.C + ve - 1) / ve;  // pieces
-  if (vec) {
+// `align`: every row of every tensor starts at, and C is, a multiple of so many elements.
+inline NormPlan norm_plan(const mita_norm_cfg_t &c, int align) {
+  const int full = 16 / (int)elem_bytes(c);
+  const int ve = align % full == 0 ? full : align % 2 == 0 ? 2 : 1;
+  const int n = c.C / ve;  // pieces
+  if (ve == full) {
     // within a wave: the fewest idle lanes (768 bf16 elements: 32 threads of three
     // pieces), then the fewest registers
-    static const int g[9][2] = {{8, 1}, {16, 1}, {32, 1}, {16, 3}, {64, 1}, {32, 3}, {64, 2}, {64, 3}, {64, 4}};
+    static const int g[12][2] = {{8, 1},  {16, 1}, {32, 1}, {16, 3},  {64, 1},  {32, 3},
+                                 {64, 2}, {64, 3}, {64, 4}, {256, 2}, {256, 4}, {1024, 2}};
     for (const auto &x : g)
       if (n <= x[0] * x[1]) return {ve, x[0], x[1]};
-    for (int p = 2; p <= 8; p *= 2)
-      if (n <= 256 * p) return {ve, 256, p};
   } else {
-    for (int p : {2, 8})
-      if (n <= 64 * p) return {ve, 64, p};
-    for (int p : {4, 16})
-      if (n <= 256 * p) return {ve, 256, p};
+    static const int g[7][2] = {{64, 2}, {64, 4}, {64, 6}, {64, 8}, {256, 4}, {256, 8}, {1024, 8}};
+    for (const auto &x : g)
+      if (n <= x[0] * x[1]) return {ve, x[0], x[1]};
   }
   return {ve, 256, 0};
 }
 // Workgroups of the backward, each with a partial sum of dw and db: two per CU,
 // or fewer where the rows do not fill them.
 inline int norm_bwd_blocks(const mita_norm_cfg_t &c, const NormPlan &p) {
-  const int64_t per = p.p ? NORM_BWD_THREADS / p.tpr : 64;
+  const int64_t per = p.p ? std::max(1, NORM_BWD_THREADS / p.tpr) : 64;
   return (int)std::min<int64_t>((norm_rows(c) + per - 1) / per, 2 * CUS);
 }
 inline size_t norm_workspace_size(const mita_norm_cfg_t *c) {
   if (check_norm(c, nullptr) != MITA_OK) return 0;
-  // whether rows can be read 16 bytes at a time is known only with the pointers
-  const int n = std::max(norm_bwd_blocks(*c, norm_plan(*c, true)), norm_bwd_blocks(*c, norm_plan(*c, false)));
+  // how rows are aligned is known only with the pointers
+  int n = 0;
+  for (int align = 1; align <= 8; align *= 2)
+    if (c->C % align == 0) n = std::max(n, norm_bwd_blocks(*c, norm_plan(*c, align)));
   return align_up((size_t)n * 2 * c->C * sizeof(float));
 }
 

@@ -51,19 +51,37 @@ __device__ __forceinline__ int64_t row_at(const NormArgs &a, const NormRows &s, 
 template <typename T, int VE> struct Piece;
 template <typename T> struct Piece<T, 16 / sizeof(T)> {
   uint4 v;
-  __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
   __device__ __forceinline__ void load(const T *p) { v = *reinterpret_cast<const uint4 *>(p); }
   __device__ __forceinline__ void get(float *f) const { unpack16(v, f, (const T *)nullptr); }
 };
+template <> struct Piece<bf16_t, 2> {
+  uint32_t v;
+  __device__ __forceinline__ void load(const bf16_t *p) { v = *reinterpret_cast<const uint32_t *>(p); }
+  __device__ __forceinline__ void get(float *f) const {
+    f[0] = __uint_as_float(v << 16);
+    f[1] = __uint_as_float(v & 0xffff0000u);
+  }
+};
+template <> struct Piece<float, 2> {
+  float2 v;
+  __device__ __forceinline__ void load(const float *p) { v = *reinterpret_cast<const float2 *>(p); }
+  __device__ __forceinline__ void get(float *f) const {
+    f[0] = v.x;
+    f[1] = v.y;
+  }
+};
 template <typename T> struct Piece<T, 1> {
   T v;
-  __device__ __forceinline__ void zero() { v = from_f32<T>(0.f); }
   __device__ __forceinline__ void load(const T *p) { v = *p; }
   __device__ __forceinline__ void get(float *f) const { f[0] = to_f32(v); }
 };
 template <typename T, int VE> __device__ __forceinline__ void put(T *p, const float *f) {
   if constexpr (VE == 1) {
     *p = from_f32<T>(f[0]);
+  } else if constexpr (VE == 2 && sizeof(T) == 4) {
+    *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
+  } else if constexpr (VE == 2) {
+    *reinterpret_cast<uint32_t *>(p) = pack_bf16x2(f[0], f[1]);
   } else if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
   } else {
@@ -137,33 +155,46 @@ template <int W> __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
-// Sums over the TPR threads of a row. Those of a workgroup's four-wave parts go
-// through `red`, whose halves consecutive calls use in turn.
-template <int TPR, int K> __device__ __forceinline__ void row_sum(float (&x)[K], float (*red)[4][K], int &turn) {
+// Sums over the TPR threads of a row. Those of several waves go through `red`,
+// whose halves consecutive calls use in turn.
+template <int TPR, int THREADS, int K> struct RowSum {
+  static constexpr int W = TPR > 64 ? TPR / 64 : 1, ROWS = THREADS / TPR;
+  float (*red)[ROWS][W][K];  // [2]
+  int turn = 0;
+  __device__ __forceinline__ void operator()(float (&x)[K]) {
 #pragma unroll
-  for (int k = 0; k < K; ++k) x[k] = group_sum < TPR<64 ? TPR : 64>(x[k]);
-  if constexpr (TPR > 64) {
-    const int sub = threadIdx.x / TPR, w = (threadIdx.x % TPR) >> 6;
-    float(*r)[K] = red[4 * turn + sub];
-    turn ^= 1;
-    if ((threadIdx.x & 63) == 0) {
+    for (int k = 0; k < K; ++k) x[k] = group_sum<(TPR < 64 ? TPR : 64)>(x[k]);
+    if constexpr (W > 1) {
+      const int sub = threadIdx.x / TPR, w = (threadIdx.x % TPR) >> 6;
+      float(*r)[K] = red[turn][sub];
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) r[w][k] = x[k];
+        for (int k = 0; k < K; ++k) r[w][k] = x[k];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float y = r[0][k];
+#pragma unroll
+        for (int i = 1; i < W; ++i) y += r[i][k];
+        x[k] = y;
+      }
     }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = (r[0][k] + r[1][k]) + (r[2][k] + r[3][k]);
   }
-}
+};
 
 // U rows per thread group, all loaded before the first is reduced; a workgroup
 // does not go on to others: nothing would wait for its stores, but the next loads
 // would (loads and stores share one counter).
+template <int TPR> constexpr int fwd_threads = TPR > NORM_FWD_THREADS ? TPR : NORM_FWD_THREADS;
+template <int TPR> constexpr int bwd_threads = TPR > NORM_BWD_THREADS ? TPR : NORM_BWD_THREADS;
 template <typename T, int VE, int TPR, int P, int U>
-__global__ void __launch_bounds__(NORM_FWD_THREADS) norm_fwd_kernel(NormArgs a) {
-  constexpr int RPB = NORM_FWD_THREADS / TPR;
-  __shared__ float red[8][4][1];
-  int turn = 0;
+__global__ void __launch_bounds__(fwd_threads<TPR>) norm_fwd_kernel(NormArgs a) {
+  using Sum = RowSum<TPR, fwd_threads<TPR>, 1>;
+  constexpr int RPB = Sum::ROWS;
+  __shared__ float red[2][Sum::ROWS][Sum::W][1];
+  Sum row_sum{red};
   const int t = threadIdx.x % TPR, r0 = blockIdx.x * RPB * U + threadIdx.x / TPR;
   RowRegs<T, VE, TPR, P> x[U];
 #pragma unroll
@@ -182,7 +213,7 @@ __global__ void __launch_bounds__(NORM_FWD_THREADS) norm_fwd_kernel(NormArgs a) 
 #pragma unroll
       for (int e = 0; e < VE; ++e) sum[0] += v[j][e];
     }
-    row_sum<TPR>(sum, red, turn);
+    row_sum(sum);
     const float mean = sum[0] * a.invC;
     float var[1] = {0.f};
 #pragma unroll
@@ -194,7 +225,7 @@ __global__ void __launch_bounds__(NORM_FWD_THREADS) norm_fwd_kernel(NormArgs a) 
         var[0] = __builtin_fmaf(v[j][e], v[j][e], var[0]);
       }
     }
-    row_sum<TPR>(var, red, turn);
+    row_sum(var);
     const float rstd = 1.f / sqrtf(var[0] * a.invC + a.eps);
     if (r < a.rows) {
       T *y = (T *)a.y + row_at(a, a.sy, r);
@@ -218,11 +249,12 @@ __global__ void __launch_bounds__(NORM_FWD_THREADS) norm_fwd_kernel(NormArgs a) 
 // WG: are dw and db wanted? A workgroup goes over rows gridDim.x * RPB apart and
 // keeps its columns' sums.
 template <typename T, int VE, int TPR, int P, bool WG>
-__global__ void __launch_bounds__(NORM_BWD_THREADS) norm_bwd_kernel(NormArgs a) {
-  constexpr int RPB = NORM_BWD_THREADS / TPR;
-  __shared__ float red[8][4][2];
-  __shared__ float sums[WG ? NORM_BWD_THREADS * VE : 1];
-  int turn = 0;
+__global__ void __launch_bounds__(bwd_threads<TPR>) norm_bwd_kernel(NormArgs a) {
+  using Sum = RowSum<TPR, bwd_threads<TPR>, 2>;
+  constexpr int RPB = Sum::ROWS;
+  __shared__ float red[2][Sum::ROWS][Sum::W][2];
+  __shared__ float sums[WG ? bwd_threads<TPR> * VE : 1];
+  Sum row_sum{red};
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float w[P][VE], dw[P][VE], db[P][VE];
   weights<VE, TPR, P>(w, a.w, a.w16, a.C, t, 1.f);
@@ -260,7 +292,7 @@ __global__ void __launch_bounds__(NORM_BWD_THREADS) norm_bwd_kernel(NormArgs a) 
       }
     }
     if (!a.dx) continue;
-    row_sum<TPR>(sm, red, turn);
+    row_sum(sm);
     const float s1 = sm[0] * a.invC, s2 = sm[1] * a.invC;
     if (r < a.rows) {
       T *dx = (T *)a.dx + row_at(a, a.sdx, r);
@@ -290,7 +322,7 @@ __global__ void __launch_bounds__(NORM_BWD_THREADS) norm_bwd_kernel(NormArgs a) 
 #pragma unroll
         for (int e = 0; e < VE; ++e) sums[threadIdx.x * VE + e] = k ? db[j][e] : dw[j][e];
         __syncthreads();
-        for (int c = threadIdx.x; c < TPR * VE; c += NORM_BWD_THREADS) {
+        for (int c = threadIdx.x; c < TPR * VE; c += bwd_threads<TPR>) {
           const int i = j * TPR * VE + c;
           if (i < a.C) {
             float y = 0.f;
@@ -404,14 +436,17 @@ template <typename T> __global__ void __launch_bounds__(512) norm_dw_wide_kernel
   part[a.C + i] = db;
 }
 
-bool row_vectors(const mita_norm_cfg_t &c, const Strided &s, const void *p) {
-  const int64_t ve = 16 / (int64_t)elem_bytes(c);
-  if (!p) return true;
-  if (c.C % ve != 0 || ((uintptr_t)p & 15)) return false;
-  for (int i = 0; i < 3; ++i)
-    if (s.n[i] > 1 && s.s[i] % ve != 0) return false;
-  return true;
+// The largest power of two up to 16 bytes, in elements, that divides the width and
+// every row's place.
+int row_align(const mita_norm_cfg_t &c, const Strided &s, const void *p, int align) {
+  if (!p) return align;
+  auto divides = [&](int64_t v) { return c.C % v == 0 && (uintptr_t)p % (v * elem_bytes(c)) == 0 &&
+                                         (s.n[0] == 1 || s.s[0] % v == 0) && (s.n[1] == 1 || s.s[1] % v == 0) &&
+                                         (s.n[2] == 1 || s.s[2] % v == 0); };
+  while (align > 1 && !divides(align)) align /= 2;
+  return align;
 }
+
 // The arguments of a call on `tensors` strided tensors, whose distances go to
 // `to`; the statistics come last. The walk goes over the dimensions in the order of
 // the first tensor's distances.
@@ -450,25 +485,33 @@ NormArgs norm_args(const mita_norm_cfg_t &c, const Strided *t, int tensors, Norm
 
 template <typename T, int VE, int TPR, int P> hipError_t fwd_p(const NormArgs &a, hipStream_t st) {
   // as many rows per thread as give four pieces, once that leaves eight workgroups per CU
-  constexpr int RPB = NORM_FWD_THREADS / TPR, U = P >= 4 ? 1 : P >= 2 ? 2 : 4;
+  constexpr int N = fwd_threads<TPR>, RPB = N / TPR, U = P >= 4 ? 1 : P >= 2 ? 2 : 4;
   if (U > 1 && a.rows >= RPB * U * 8 * CUS)
-    norm_fwd_kernel<T, VE, TPR, P, U><<<dim3((unsigned)((a.rows + RPB * U - 1) / (RPB * U))), NORM_FWD_THREADS, 0, st>>>(a);
+    norm_fwd_kernel<T, VE, TPR, P, U><<<dim3((unsigned)((a.rows + RPB * U - 1) / (RPB * U))), N, 0, st>>>(a);
   else
-    norm_fwd_kernel<T, VE, TPR, P, 1><<<dim3((unsigned)((a.rows + RPB - 1) / RPB)), NORM_FWD_THREADS, 0, st>>>(a);
+    norm_fwd_kernel<T, VE, TPR, P, 1><<<dim3((unsigned)((a.rows + RPB - 1) / RPB)), N, 0, st>>>(a);
   return launched("norm_fwd_kernel", st);
 }
 template <typename T, int VE, int TPR, int P> hipError_t bwd_p(const NormArgs &a, int blocks, hipStream_t st) {
   if (a.dw || a.db)
-    norm_bwd_kernel<T, VE, TPR, P, true><<<dim3((unsigned)blocks), NORM_BWD_THREADS, 0, st>>>(a);
+    norm_bwd_kernel<T, VE, TPR, P, true><<<dim3((unsigned)blocks), bwd_threads<TPR>, 0, st>>>(a);
   else
-    norm_bwd_kernel<T, VE, TPR, P, false><<<dim3((unsigned)blocks), NORM_BWD_THREADS, 0, st>>>(a);
+    norm_bwd_kernel<T, VE, TPR, P, false><<<dim3((unsigned)blocks), bwd_threads<TPR>, 0, st>>>(a);
   return launched("norm_bwd_kernel", st);
 }
 
 // f.run<VE, TPR, P>() for the plan's geometry
+template <int VE, typename F> hipError_t with_plan_odd(const NormPlan &p, F &f) {
+  if (p.tpr == 64) {
+    if (p.p <= 4) return p.p == 2 ? f.template run<VE, 64, 2>() : f.template run<VE, 64, 4>();
+    return p.p == 6 ? f.template run<VE, 64, 6>() : f.template run<VE, 64, 8>();
+  }
+  if (p.tpr == 256) return p.p == 4 ? f.template run<VE, 256, 4>() : f.template run<VE, 256, 8>();
+  return f.template run<VE, 1024, 8>();
+}
 template <typename T, typename F> hipError_t with_plan(const NormPlan &p, F &&f) {
   constexpr int V = 16 / (int)sizeof(T);
-  if (p.ve > 1) {
+  if (p.ve == V) {
     if (p.tpr == 8) return f.template run<V, 8, 1>();
     if (p.tpr == 16) return p.p == 1 ? f.template run<V, 16, 1>() : f.template run<V, 16, 3>();
     if (p.tpr == 32) return p.p == 1 ? f.template run<V, 32, 1>() : f.template run<V, 32, 3>();
@@ -478,12 +521,10 @@ template <typename T, typename F> hipError_t with_plan(const NormPlan &p, F &&f)
       if (p.p == 3) return f.template run<V, 64, 3>();
       return f.template run<V, 64, 4>();
     }
-    if (p.p == 2) return f.template run<V, 256, 2>();
-    if (p.p == 4) return f.template run<V, 256, 4>();
-    return f.template run<V, 256, 8>();
+    if (p.tpr == 256) return p.p == 2 ? f.template run<V, 256, 2>() : f.template run<V, 256, 4>();
+    return f.template run<V, 1024, 2>();
   }
-  if (p.tpr == 64) return p.p == 2 ? f.template run<1, 64, 2>() : f.template run<1, 64, 8>();
-  return p.p == 4 ? f.template run<1, 256, 4>() : f.template run<1, 256, 16>();
+  return p.ve == 2 ? with_plan_odd<2>(p, f) : with_plan_odd<1>(p, f);
 }
 template <typename T> struct RunFwd {
   const NormArgs &a;
@@ -538,7 +579,7 @@ hipError_t launch_norm_forward(const mita_norm_cfg_t &c, const void *x, const vo
   a.y = y;
   a.mean = mean;
   a.rstd = rstd;
-  const NormPlan p = norm_plan(c, row_vectors(c, t[0], x) && row_vectors(c, t[1], y));
+  const NormPlan p = norm_plan(c, row_align(c, t[1], y, row_align(c, t[0], x, 16 / (int)elem_bytes(c))));
   return c.dtype == MITA_F32 ? forward_t<float>(a, p, st) : forward_t<bf16_t>(a, p, st);
 }
 
@@ -557,7 +598,7 @@ hipError_t launch_norm_backward(const mita_norm_cfg_t &c, const void *x, const v
   a.dw = dw;
   a.db = db;
   a.part = (float *)ws;
-  const NormPlan p = norm_plan(c, row_vectors(c, t[0], x) && row_vectors(c, t[1], dy) && row_vectors(c, t[2], dx));
+  const NormPlan p = norm_plan(c, row_align(c, t[2], dx, row_align(c, t[1], dy, row_align(c, t[0], x, 16 / (int)elem_bytes(c)))));
   const int blocks = norm_bwd_blocks(c, p);
   return c.dtype == MITA_F32 ? backward_t<float>(a, p, blocks, st) : backward_t<bf16_t>(a, p, blocks, st);
 }

@@ -136,11 +136,12 @@ int main() {
   CHECK(check_norm(&m, nullptr) == MITA_OK);
   for (int C = 1; C <= MITA_NORM_MAX_C; C = C < 20000 ? C + 1 : C * 2)
     for (int t : {MITA_F32, MITA_BF16})
-      for (bool vec : {false, true}) {
+      for (int align : {1, 2, 4, 8}) {
         mita_norm_cfg_t x = m;
         x.C = C, x.dtype = t;
-        if (vec && C % (16 / (int)elem_bytes(x))) continue;
-        const NormPlan p = norm_plan(x, vec);
+        if (C % align) continue;
+        const NormPlan p = norm_plan(x, align);
+        CHECK(align % p.ve == 0);
         if (p.p) CHECK((int64_t)p.ve * p.tpr * p.p >= C);
         CHECK(norm_workspace_size(&x) >= (size_t)norm_bwd_blocks(x, p) * 2 * C * 4);
       }
