@@ -16,8 +16,12 @@ sample of the same workload. Details go to stderr.
 
 --dense runs the dense reference on the same inputs instead: route-only with
 one landmark and k = N, so every query attends over every key (full softmax
-attention) on the same kernels; PyTorch's flash SDPA is timed beside it as
-context.
+attention) on the same kernels; the library's dense attention (with --backward
+its gradients too) and PyTorch's flash SDPA are timed beside it as context.
+
+--qk-norm normalises the queries and keys of every head (layer norm over d)
+as part of every step, and with --backward takes the gradients back through
+it.
 """
 from __future__ import annotations
 
@@ -241,6 +245,40 @@ def sdpa_ms(q, k, v, steps, warmup):
         return None
 
 
+def dense_ms(wl, q, k, v, dO, steps, warmup):
+    """The library's dense attention on the same tensors: (forward ms, forward +
+    backward ms or None without dO)."""
+    import torch
+    from paper_2602_01219_amd import mita
+    cfg = mita.DenseConfig(B=wl.B, H=wl.H, N=wl.N, d=wl.d, dtype=wl.dtype)
+    ws = [torch.empty(max(1, mita.dense_workspace_size(cfg, w)), dtype=torch.uint8, device="cuda")
+          for w in (mita.WS_FORWARD, mita.WS_BACKWARD)]
+    o, lse = mita.dense_forward(cfg, q, k, v, ws=ws[0])
+    grads = tuple(torch.empty_like(x) for x in (q, k, v))
+
+    def forward():
+        mita.dense_forward(cfg, q, k, v, o=o, lse=lse, ws=ws[0])
+
+    def both():
+        forward()
+        mita.dense_backward(cfg, q, k, v, o, lse, dO, dq=grads[0], dk=grads[1], dv=grads[2], ws=ws[1])
+
+    out = []
+    for step in (forward, both if dO is not None else None):
+        if step is None:
+            out.append(None)
+            continue
+        for _ in range(warmup):
+            step()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(steps):
+            step()
+        torch.cuda.synchronize()
+        out.append((time.perf_counter() - t0) * 1e3 / steps)
+    return tuple(out)
+
+
 def run(wl, name, a, dense: bool):
     import numpy as np
     import torch
@@ -276,6 +314,23 @@ def run(wl, name, a, dense: bool):
         ws_t = (torch.empty(mita.workspace_size(cfg, mita.WS_TOME), dtype=torch.uint8, device="cuda")
                 if tome_lm else None)
 
+    if a.qk_norm:
+        # q and k as projected; the step normalises them into q and k
+        ncfg = mita.NormConfig((wl.B, wl.H, wl.N), wl.d, dtype=wl.dtype)
+        raw = (q, k)
+        q, k = torch.empty_like(q), torch.empty_like(k)
+        gain, bias = torch.ones(wl.d, device="cuda"), torch.zeros(wl.d, device="cuda")
+        stats = [[torch.empty((wl.B, wl.H, wl.N), device="cuda") for _ in range(2)] for _ in raw]
+        ws_n = torch.empty(mita.norm_workspace_size(ncfg), dtype=torch.uint8, device="cuda")
+
+    def normalise():
+        for x, y, (mean, rstd) in zip(raw, (q, k), stats):
+            mita.norm_forward(ncfg, x, gain, bias, y=y, mean=mean, rstd=rstd)
+
+    def normalise_backward():
+        for x, g, (mean, rstd) in zip(raw, grads, stats):
+            mita.norm_backward(ncfg, x, mean, rstd, g, gain, dx=g, ws=ws_n)
+
     def make_landmarks():
         if random_lm:
             mita.landmarks_select(cfg, q, sel, q_lm=q_lm)
@@ -292,9 +347,13 @@ def run(wl, name, a, dense: bool):
         eprint(f"[bench] backward workspace {ws_b.numel() / 2**20:.1f} MiB")
 
     def step(timer=None, timer_b=None):
+        if a.qk_norm:
+            normalise()
         if a.backward:
             mita.forward(cfg, q, k, v, o=o, ws=ws, timer=timer)
             mita.backward(cfg, q, k, v, o, dO, *grads, ws=ws_b, timer=timer_b)
+            if a.qk_norm:
+                normalise_backward()
             return
         if random_lm or tome_lm:
             make_landmarks()
@@ -359,6 +418,7 @@ def run(wl, name, a, dense: bool):
     sdpa = None
     if dense:
         sdpa = sdpa_ms(q, k, v, a.steps, a.warmup)
+        own_ms = dense_ms(wl, q, k, v, dO if a.backward else None, a.steps, a.warmup)
     if a.calib_copy_mib:
         # a plain elementwise kernel that reads and writes calib_copy_mib MiB
         # each (torch's copy_ of contiguous tensors is a runtime blit, whose
@@ -451,6 +511,7 @@ def run(wl, name, a, dense: bool):
                    "use_shared": wl.use_shared, "use_routed": wl.use_routed,
                    "gather": "staged" if a.staged_gather else "in-place",
                    "select": "fused" if plan["fused"] else "full-scores", "s": s_exp, "landmarks": a.landmarks,
+                   **({"qk_norm": True} if a.qk_norm else {}),
                    "parallelism": "none (1 GPU)"},
         "roofline": roofline,
         "cpu_baseline": cpu,
@@ -463,6 +524,9 @@ def run(wl, name, a, dense: bool):
     }
     if dense:
         out["sdpa_flash_ms"] = None if sdpa is None else round(sdpa, 4)
+        out["dense_attention_ms"] = round(own_ms[0], 4)
+        if own_ms[1] is not None:
+            out["dense_attention_train_ms"] = round(own_ms[1], 4)
     return out
 
 
@@ -484,6 +548,8 @@ def main():
                     help="time forward + backward steps (gradients of q, k, v for a synthetic upstream gradient)")
     ap.add_argument("--landmarks", choices=("pool", "random", "tome"), default="pool",
                     help="landmark extraction: 2-D pooling (default), random selection or token merging (Tab. A1)")
+    ap.add_argument("--qk-norm", action="store_true",
+                    help="layer norm of every head's queries and keys as part of the step")
     ap.add_argument("--cpu-budget", type=float, default=12.0,
                     help="seconds of float32 oracle time for cpu_baseline (half as much again in float64)")
     ap.add_argument("--no-cpu-baseline", action="store_true")

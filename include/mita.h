@@ -350,7 +350,8 @@ typedef struct {
  * p - left <= j <= p + right (left, right = -1: no bound; right = 0: causal).
  */
 typedef struct {
-  int32_t B, H, H_kv;      /* batch, query heads, key/value heads; H_kv divides H */
+  int32_t B, H, H_kv;      /* batch, query heads (at most 4096), key/value heads; H_kv divides H; N * H / H_kv
+                              at most 2^27 (MITA_ERR_UNSUPPORTED beyond) */
   int32_t N, N_k, d;       /* queries, keys (each in [1, MITA_DENSE_MAX_N]), head dim in {64, 128} */
   int32_t dtype;           /* MITA_F32 or MITA_BF16: storage of all tensors but the log-sum-exps */
   int32_t left, right;     /* window, -1 for no bound */

@@ -10,6 +10,7 @@ calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -582,6 +583,16 @@ def _plan_for(cfg, kind, ts, make):
     return plan
 
 
+_NOW = contextlib.nullcontext()
+
+
+def _on(plan, stream):
+    """A call's own allocations belong to the stream it is given."""
+    if stream.device != plan.device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {plan.device}")
+    return torch.cuda.stream(stream)
+
+
 def _ws_for(plan, ws):
     if ws is None:
         if not plan.need:
@@ -594,12 +605,7 @@ def _ws_for(plan, ws):
 
 def _call(plan, fn, args, stream):
     """fn(cfg, *args, stream) with the tensors' device current."""
-    if stream is None:
-        raw = torch._C._cuda_getCurrentRawStream(plan.index)
-    else:
-        if stream.device != plan.device:
-            raise ValueError(f"the stream is on {stream.device}, the tensors on {plan.device}")
-        raw = stream.cuda_stream
+    raw = torch._C._cuda_getCurrentRawStream(plan.index) if stream is None else stream.cuda_stream
     if torch.cuda.current_device() == plan.index:
         st = fn(plan.ref, *args, raw)
     else:
@@ -644,10 +650,11 @@ def dense_forward(cfg: DenseConfig, q, k, v, q_len=None, k_len=None, o=None, lse
     are [B] int32 device tensors."""
     lib = load_library()
     plan = _plan_for(cfg, "forward", (q, k, v, q_len, k_len, o, lse), _dense_forward_plan)
-    o = plan.out(o, 0)
-    if lse is None and want_lse:
-        lse = plan.new(1)
-    ws, wp, wn = _ws_for(plan, ws)
+    with _NOW if stream is None else _on(plan, stream):
+        o = plan.out(o, 0)
+        if lse is None and want_lse:
+            lse = plan.new(1)
+        ws, wp, wn = _ws_for(plan, ws)
     _call(plan, lib.mita_dense_forward, (q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_len), _ptr(k_len),
                                          o.data_ptr(), _ptr(lse), wp, wn), stream)
     return o, lse
@@ -676,8 +683,9 @@ def dense_backward(cfg: DenseConfig, q, k, v, o, lse, dO, q_len=None, k_len=None
     (mita_dense_backward)."""
     lib = load_library()
     plan = _plan_for(cfg, "backward", (q, k, v, o, lse, dO, q_len, k_len, dq, dk, dv), _dense_backward_plan)
-    dq, dk, dv = plan.out(dq, 0), plan.out(dk, 1), plan.out(dv, 2)
-    ws, wp, wn = _ws_for(plan, ws)
+    with _NOW if stream is None else _on(plan, stream):
+        dq, dk, dv = plan.out(dq, 0), plan.out(dk, 1), plan.out(dv, 2)
+        ws, wp, wn = _ws_for(plan, ws)
     _call(plan, lib.mita_dense_backward, (q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
                                           dO.data_ptr(), _ptr(q_len), _ptr(k_len), dq.data_ptr(), dk.data_ptr(),
                                           dv.data_ptr(), wp, wn), stream)
@@ -714,9 +722,10 @@ def norm_forward(cfg: NormConfig, x, w=None, b=None, y=None, mean=None, rstd=Non
     None). x may be strided (its last dimension dense)."""
     lib = load_library()
     plan = _plan_for(cfg, "forward", (x, w, b, y, mean, rstd), _norm_forward_plan)
-    y = plan.out(y, 0)
-    if want_stats:
-        mean, rstd = plan.out(mean, 1), plan.out(rstd, 1)
+    with _NOW if stream is None else _on(plan, stream):
+        y = plan.out(y, 0)
+        if want_stats:
+            mean, rstd = plan.out(mean, 1), plan.out(rstd, 1)
     _call(plan, lib.mita_norm_forward, (x.data_ptr(), _ptr(w), _ptr(b), y.data_ptr(), _ptr(mean), _ptr(rstd)), stream)
     return y, mean, rstd
 
@@ -744,11 +753,12 @@ def norm_backward(cfg: NormConfig, x, mean, rstd, dy, w=None, dx=None, dw=None, 
     db, are None unless wanted."""
     lib = load_library()
     plan = _plan_for(cfg, "backward", (x, mean, rstd, dy, w, dx, dw, db), _norm_backward_plan)
-    if want_dx:
-        dx = plan.out(dx, 0)
-    if want_weights:
-        dw, db = plan.out(dw, 1), plan.out(db, 1)
-    ws, wp, wn = _ws_for(plan, ws) if dw is not None or db is not None else (None, None, 0)
+    with _NOW if stream is None else _on(plan, stream):
+        if want_dx:
+            dx = plan.out(dx, 0)
+        if want_weights:
+            dw, db = plan.out(dw, 1), plan.out(db, 1)
+        ws, wp, wn = _ws_for(plan, ws) if dw is not None or db is not None else (None, None, 0)
     _call(plan, lib.mita_norm_backward, (x.data_ptr(), _ptr(w), mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(),
                                          _ptr(dx), _ptr(dw), _ptr(db), wp, wn), stream)
     return dx, dw, db

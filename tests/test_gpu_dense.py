@@ -2,7 +2,8 @@
 (tests/dense_reference.py, whose bounds the errors are measured in)."""
 from __future__ import annotations
 
-import math
+import copy
+import pickle
 
 import pytest
 import torch
@@ -177,6 +178,47 @@ def test_offsets_past_32_bits():
     assert torch.equal(dk, dk2) and torch.equal(dv, dv2)
     R = reference(cfg, q, k, v, dO=dO, o=o, lse=lse)
     assert max(worst(o, R.o, R.eo), worst(dk, R.dk, R.edk), worst(dv, R.dv, R.edv)) <= 1.0
+
+
+def test_grouped_heads_4_gib_apart():
+    # two query heads of one key head, their rows 2^31 elements apart
+    N = 70
+    cfg = mita.DenseConfig(1, 2, N, 64, H_kv=1, right=0)
+    g = gen(15)
+    buf = torch.empty(2 ** 31 + N * 64, dtype=torch.bfloat16, device="cuda")
+    q = buf.as_strided((1, 2, N, 64), (2 ** 32, 2 ** 31, 64, 1))
+    q.copy_(heads(g, 1, 2, N, 64, torch.bfloat16, "bhnd"))
+    k, v = (heads(g, 1, 1, N, 64, torch.bfloat16, "bhnd") for _ in range(2))
+    dO = heads(g, 1, 2, N, 64, torch.bfloat16, "bhnd")
+    o, lse = mita.dense_forward(cfg, q, k, v)
+    near = q.contiguous()
+    o2, lse2 = mita.dense_forward(cfg, near, k, v)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    far = mita.dense_backward(cfg, q, k, v, o, lse, dO, dq=torch.empty_like(near))
+    assert all(torch.equal(x, y) for x, y in zip(far, mita.dense_backward(cfg, near, k, v, o, lse, dO)))
+
+
+def test_configurations_copy_and_pickle_after_use():
+    cfg = mita.DenseConfig(1, 1, 3, 64)
+    g = gen(16)
+    x = heads(g, 1, 1, 3, 64, torch.bfloat16, "bhnd")
+    mita.dense_forward(cfg, x, x.clone(), x.clone())
+    for other in (copy.deepcopy(cfg), pickle.loads(pickle.dumps(cfg))):
+        assert other == cfg and "_plans" not in other.__dict__
+
+
+def test_a_stream_of_its_own_without_given_outputs():
+    # the call's allocations belong to the stream it runs on
+    cfg = mita.DenseConfig(2, 2, 64, 64, N_k=2048)
+    g = gen(17)
+    q = heads(g, 2, 2, 64, 64, torch.bfloat16, "bhnd")
+    k, v = (heads(g, 2, 2, 2048, 64, torch.bfloat16, "bhnd") for _ in range(2))
+    ref = mita.dense_forward(cfg, q, k, v)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [mita.dense_forward(cfg, q, k, v, stream=side) for _ in range(20)]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for o in got for a, b in zip(o, ref))
 
 
 def test_gradient_against_differences():
