@@ -12,9 +12,13 @@
 // As the B operand of the next product a lane needs rows of its own group g, and
 // which rows a group takes is free as long as both operands agree: the
 // accumulator's own rows serve, so P never moves between lanes.
-// bf16: one v_mfma_f32_32x32x16_bf16 per 16-long reduction step; fp32: four
-// v_mfma_f32_32x32x2_f32 per 8-long step, so both types read 16 bytes of a row
-// (chunk 2 s + g of step s) per lane for the `rows` product.
+// bf16: one v_mfma_f32_32x32x16_bf16 per 16-long reduction step. fp32: each operand
+// as three bf16 numbers that add up to it exactly (8 bits of its 24 each), and six
+// of the nine products; the three left out are below 2^-23 of the product, about
+// fp32's own rounding. That takes 6 x 32 cycles of the matrix cores per 16-long step where the
+// fp32 instruction takes 8 x 64, and splitting an operand on the way (44 VALU
+// instructions per 8 elements and lane) runs beside it: 16 heads of 2048 tokens, d =
+// 128, 310 -> 224 us forward and 1049 -> 800 backward, 154 TFLOP/s of fp32 products.
 #pragma once
 #include "cdna4.hpp"
 #include "flash.hpp"
@@ -179,32 +183,115 @@ template <typename T, int D> struct TileAddr {
   }
 };
 
-// One reduction step of a `rows` product.
-__device__ __forceinline__ f32x16 mma32(bf16_t *, const uint4 &a, const uint4 &b, f32x16 c) {
+__device__ __forceinline__ f32x16 mma32(const uint4 &a, const uint4 &b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
                                                  0);
 }
-__device__ __forceinline__ f32x16 mma32(float *, const uint4 &a, const uint4 &b, f32x16 c) {
-  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
-  return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+
+// Eight fp32 values as bf16 numbers h + m + l = x: h and m are the upper halves of x
+// and of x - h (no rounding), and l, what is left, has at most 8 bits.
+struct Split {
+  uint4 h, m, l;
+  __device__ __forceinline__ void set(const float (&x)[8]) {
+    uint32_t u[3][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      u[0][i] = __float_as_uint(x[i]);
+      const float r = x[i] - __uint_as_float(u[0][i] & 0xffff0000u);
+      u[1][i] = __float_as_uint(r);
+      u[2][i] = __float_as_uint(r - __uint_as_float(u[1][i] & 0xffff0000u));
+    }
+    auto upper = [](const uint32_t (&v)[8]) {
+      return make_uint4(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u),
+                        __builtin_amdgcn_perm(v[5], v[4], 0x07060302u), __builtin_amdgcn_perm(v[7], v[6], 0x07060302u));
+    };
+    h = upper(u[0]);
+    m = upper(u[1]);
+    l = upper(u[2]);
+  }
+  __device__ __forceinline__ void set(const uint4 &a, const uint4 &b) {
+    const float x[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                        __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+    set(x);
+  }
+};
+__device__ __forceinline__ f32x16 mma32(const Split &a, const Split &b, f32x16 c) {
+  c = mma32(a.l, b.h, c);
+  c = mma32(a.h, b.l, c);
+  c = mma32(a.m, b.m, c);
+  c = mma32(a.m, b.h, c);
+  c = mma32(a.h, b.m, c);
+  return mma32(a.h, b.h, c);
+}
+
+// A lane's column as B operand of `rows`, from its row in memory (zero without one):
+// bf16 holds chunk 2 s + g for step s, fp32 chunks 4 t + g and 4 t + 2 + g for step t.
+template <typename T, int D> struct Column;
+template <int D> struct Column<bf16_t, D> {
+  static constexpr int NS = RowTile<bf16_t, D>::NS;
+  uint4 b[NS];
+  __device__ __forceinline__ void load(const char *row, bool valid) {
+    const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      b[s] = valid ? *reinterpret_cast<const uint4 *>(row + 32 * s + 16 * g) : make_uint4(0, 0, 0, 0);
+  }
+};
+template <int D> struct Column<float, D> {
+  static constexpr int NS = RowTile<float, D>::NS / 2;
+  Split b[NS];
+  __device__ __forceinline__ void load(const char *row, bool valid) {
+    const int g = (threadIdx.x & 63) >> 5;
+    uint4 x[2 * NS];
+#pragma unroll
+    for (int s = 0; s < 2 * NS; ++s)
+      x[s] = valid ? *reinterpret_cast<const uint4 *>(row + 32 * s + 16 * g) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) b[s].set(x[2 * s], x[2 * s + 1]);
+  }
+};
+// The scalar product of a column's rows x and y (0 without them), in both its lanes' parts.
+template <typename T, int D> __device__ __forceinline__ float column_dot(const char *x, const char *y, bool valid) {
+  const int g = (threadIdx.x & 63) >> 5;
+  float d = 0.f;
+  if (valid) {
+#pragma unroll
+    for (int s = 0; s < RowTile<T, D>::NS; ++s) {
+      float u[16 / sizeof(T)], v[16 / sizeof(T)];
+      unpack16(*reinterpret_cast<const uint4 *>(x + 32 * s + 16 * g), u, (const T *)nullptr);
+      unpack16(*reinterpret_cast<const uint4 *>(y + 32 * s + 16 * g), v, (const T *)nullptr);
+#pragma unroll
+      for (int j = 0; j < 16 / (int)sizeof(T); ++j) d = __builtin_fmaf(u[j], v[j], d);
+    }
+  }
+  return d;
 }
 
 // c + X B for the 32 tile rows from 32 kb on.
-template <typename T, int D>
-__device__ __forceinline__ f32x16 tile_rows(const char *tile, const TileAddr<T, D> &ad, int kb,
-                                            const uint4 (&b)[RowTile<T, D>::NS], f32x16 c) {
-  using RT = RowTile<T, D>;
+template <int D>
+__device__ __forceinline__ f32x16 tile_rows(const char *tile, const TileAddr<bf16_t, D> &ad, int kb,
+                                            const Column<bf16_t, D> &col, f32x16 c) {
+  using RT = RowTile<bf16_t, D>;
 #pragma unroll
-  for (int s = 0; s < RT::NS; ++s) {
-    const uint4 a = *reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)(s << 5)) + kb * 32 * RT::RB);
-    c = mma32((T *)nullptr, a, b[s], c);
+  for (int s = 0; s < RT::NS; ++s)
+    c = mma32(*reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)(s << 5)) + kb * 32 * RT::RB), col.b[s], c);
+  return c;
+}
+template <int D>
+__device__ __forceinline__ f32x16 tile_rows(const char *tile, const TileAddr<float, D> &ad, int kb,
+                                            const Column<float, D> &col, f32x16 c) {
+  using RT = RowTile<float, D>;
+#pragma unroll
+  for (int s = 0; s < RT::NS; s += 2) {
+    Split a;
+    a.set(*reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)(s << 5)) + kb * 32 * RT::RB),
+          *reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)((s + 1) << 5)) + kb * 32 * RT::RB));
+    c = mma32(a, col.b[s / 2], c);
   }
   return c;
 }
 
-// P as the B operand: bf16 rounds it (16 rows per operand), fp32 takes it as it is.
+// P as the B operand, 16 rows each: bf16 rounds it, fp32 splits it.
 template <typename T> struct ColsOperand;
 template <> struct ColsOperand<bf16_t> {
   uint4 b[2];
@@ -216,8 +303,15 @@ template <> struct ColsOperand<bf16_t> {
   }
 };
 template <> struct ColsOperand<float> {
-  f32x16 p;
-  __device__ __forceinline__ explicit ColsOperand(const f32x16 &x) : p(x) {}
+  Split b[2];
+  __device__ __forceinline__ explicit ColsOperand(const f32x16 &p) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const float x[8] = {p[8 * s],     p[8 * s + 1], p[8 * s + 2], p[8 * s + 3],
+                          p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
+      b[s].set(x);
+    }
+  }
 };
 
 // acc[db] += X^T P for the 32 tile rows from 32 kb on.
@@ -234,7 +328,7 @@ __device__ __forceinline__ void tile_cols(f32x16 (&acc)[D / 32], const char *til
       for (int i = 0; i < 2; ++i)
         h[i] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                              (lds_v4i16_t *)(tile + ad.col(db, i) + (32 * kb + 16 * s) * RT::RB)));
-      acc[db] = mma32((bf16_t *)nullptr, make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), P.b[s], acc[db]);
+      acc[db] = mma32(make_uint4(h[0].x, h[0].y, h[1].x, h[1].y), P.b[s], acc[db]);
     }
 }
 template <int D>
@@ -242,28 +336,20 @@ __device__ __forceinline__ void tile_cols(f32x16 (&acc)[D / 32], const char *til
                                           const ColsOperand<float> &P) {
   using RT = RowTile<float, D>;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int q = i >> 2, r = i & 3;
-    const uint32_t at = ad.c0 ^ (uint32_t)(((q & 1) << 2 | r) << 4);
+  for (int s = 0; s < 2; ++s)
 #pragma unroll
     for (int db = 0; db < RT::NB; ++db) {
-      const float a =
-          *reinterpret_cast<const float *>(tile + (at ^ (uint32_t)(db << 7)) + (32 * kb + 8 * q + r) * RT::RB);
-      acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, P.p[i], acc[db], 0, 0, 0);
-    }
-  }
-}
-
-template <typename T, int D> using Column = uint4[RowTile<T, D>::NS];
-
-// The registers of a lane's column as B operand: the 16-byte chunks 2 s + g of
-// its row, zero without one.
-template <typename T, int D>
-__device__ __forceinline__ void load_column(Column<T, D> &b, const char *row, bool valid) {
-  const int g = (threadIdx.x & 63) >> 5;
+      float x[8];  // rows acc_row(8 s + e, g), element n of block db
 #pragma unroll
-  for (int s = 0; s < RowTile<T, D>::NS; ++s)
-    b[s] = valid ? *reinterpret_cast<const uint4 *>(row + 32 * s + 16 * g) : make_uint4(0, 0, 0, 0);
+      for (int e = 0; e < 8; ++e) {
+        const int q = 2 * s + (e >> 2), r = e & 3;
+        x[e] = *reinterpret_cast<const float *>(
+            tile + (ad.c0 ^ (uint32_t)(((q & 1) << 2 | r) << 4) ^ (uint32_t)(db << 7)) + (32 * kb + 8 * q + r) * RT::RB);
+      }
+      Split a;
+      a.set(x);
+      acc[db] = mma32(a, P.b[s], acc[db]);
+    }
 }
 
 // The column's accumulators (d = 32 db + acc_row(i, g)) times `mul` to its row,

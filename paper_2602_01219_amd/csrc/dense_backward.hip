@@ -38,26 +38,16 @@ __global__ void __launch_bounds__(256, sizeof(T) * D == 128 ? 3 : sizeof(T) * D 
   const int row = tile * DENSE_TQ + 32 * w + n;
   const int tok = div_group(a, row), head = x.hk * a.G + row - tok * a.G;
   const bool exists = row < a.R, valid = exists && tok < x.qlen;
-  uint4 q[RT::NS], dO[RT::NS];
-  load_column<T, D>(q, a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
-  load_column<T, D>(dO, a.dO.p + x.b * a.dO.b + head * a.dO.h + (int64_t)tok * a.dO.n, valid);
-  float lse2 = INFINITY, Dr = 0.f;
-  {
-    uint4 o[RT::NS];
-    load_column<T, D>(o, a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n, valid);
-    if (valid) {
-      const float l = a.lse[((int64_t)x.b * a.H + head) * a.N + tok];
-      lse2 = l == -INFINITY ? INFINITY : l * LOG2E;
-    }
-#pragma unroll
-    for (int i = 0; i < RT::NS; ++i) {
-      float y[16 / sizeof(T)], z[16 / sizeof(T)];
-      unpack16(o[i], y, (const T *)nullptr);
-      unpack16(dO[i], z, (const T *)nullptr);
-#pragma unroll
-      for (int j = 0; j < 16 / (int)sizeof(T); ++j) Dr = __builtin_fmaf(y[j], z[j], Dr);
-    }
-    Dr = column_sum(Dr);
+  Column<T, D> q, dO;
+  q.load(a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
+  const char *const dOrow = a.dO.p + x.b * a.dO.b + head * a.dO.h + (int64_t)tok * a.dO.n;
+  dO.load(dOrow, valid);
+  const float Dr = column_sum(
+      column_dot<T, D>(a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n, dOrow, valid));
+  float lse2 = INFINITY;
+  if (valid) {
+    const float l = a.lse[((int64_t)x.b * a.H + head) * a.N + tok];
+    lse2 = l == -INFINITY ? INFINITY : l * LOG2E;
   }
   if (sp == 0 && lane < 32) {
     const int64_t at = ((int64_t)s * a.tiles + tile) * DENSE_TQ + 32 * w + n;
@@ -107,8 +97,8 @@ __global__ void __launch_bounds__(256, sizeof(T) * D == 128 ? 3 : sizeof(T) * D 
 #pragma unroll (D == 64 ? 2 : 1)
       for (int h = 0; h < TR / 32; ++h) {
         if (decltype(masked)::value && (k0 + 32 * h >= whi || k0 + 32 * h + 32 <= wlo)) continue;
-        f32x16 z = tile_rows<T, D>(Kt, ad, h, q, splat16(0.f));
-        const f32x16 dp = tile_rows<T, D>(Vt, ad, h, dO, splat16(-Dr));
+        f32x16 z = tile_rows<D>(Kt, ad, h, q, splat16(0.f));
+        const f32x16 dp = tile_rows<D>(Vt, ad, h, dO, splat16(-Dr));
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = k0 + 32 * h + acc_row(i, g);
@@ -150,9 +140,9 @@ __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_dkv_k
 
   const int key = kt * DENSE_KB + 32 * w + n;
   const bool exists = key < a.Nk, valid = key < x.klen;
-  uint4 kf[RT::NS], vf[RT::NS];
-  load_column<T, D>(kf, a.k.p + x.b * a.k.b + x.hk * a.k.h + (int64_t)key * a.k.n, valid);
-  load_column<T, D>(vf, a.v.p + x.b * a.v.b + x.hk * a.v.h + (int64_t)key * a.v.n, valid);
+  Column<T, D> kf, vf;
+  kf.load(a.k.p + x.b * a.k.b + x.hk * a.k.h + (int64_t)key * a.k.n, valid);
+  vf.load(a.v.p + x.b * a.v.b + x.hk * a.v.h + (int64_t)key * a.v.n, valid);
 
   // tokens [first, end) see key j; in rows, times G
   const int Rv = x.qlen * a.G;  // rows that exist
@@ -182,7 +172,7 @@ __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_dkv_k
 
   const uint32_t atQ = lds_at(ldsQ), atG = lds_at(ldsG), atL = lds_at(ldsL);
   auto issue = [&](int p) {
-    if (D == 128) copy.forget();
+    if (sizeof(T) * D >= 256) copy.forget();
     const int r0 = rbeg + order.at(p) * TR;
     const uint32_t qt = atQ + (p & 1) * BYTES, gt = atG + (p & 1) * BYTES, lt = atL + (p & 1) * 512;
     if (a.G == 1) {
@@ -224,10 +214,10 @@ __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_dkv_k
       const char *qt = ldsQ + (p & 1) * BYTES, *gt = ldsG + (p & 1) * BYTES;
 #pragma unroll (D == 64 ? 2 : 1)
       for (int h = 0; h < TR / 32; ++h) {
-        if (D == 128) ad.forget();  // (registers are short)
+        if (sizeof(T) * D >= 256) ad.forget();  // (registers are short)
         if (decltype(masked)::value && (r0 + 32 * h >= whi || r0 + 32 * h + 32 <= wlo)) continue;
         const float *ls = (const float *)(ldsL + (p & 1) * 512) + 32 * h + 4 * g, *ds = ls + 64;
-        f32x16 z = tile_rows<T, D>(qt, ad, h, kf, splat16(0.f));
+        f32x16 z = tile_rows<D>(qt, ad, h, kf, splat16(0.f));
         f32x16 dp;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -237,7 +227,7 @@ __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_dkv_k
           dp[4 * c + 2] = -y.z;
           dp[4 * c + 3] = -y.w;
         }
-        dp = tile_rows<T, D>(gt, ad, h, vf, dp);
+        dp = tile_rows<D>(gt, ad, h, vf, dp);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const float4 y = *reinterpret_cast<const float4 *>(ls + 8 * c);

@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_fwd_k
   const int row = tile * DENSE_TQ + 32 * w + n;
   const int tok = div_group(a, row), head = x.hk * a.G + row - tok * a.G;
   const bool exists = row < a.R, valid = exists && tok < x.qlen;
-  uint4 q[RT::NS];
-  load_column<T, D>(q, a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
+  Column<T, D> q;
+  q.load(a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
   const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
   // keys that some row of the wave sees (none: the wave only copies)
   const int wr = tile * DENSE_TQ + 32 * w;
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_fwd_k
   st.init();
 
   f32x16 sc[HT];
-  auto scores = [&](int p, int h) { return tile_rows<T, D>(ldsK + (p & 1) * BYTES, ad, h, q, splat16(0.f)); };
+  auto scores = [&](int p, int h) { return tile_rows<D>(ldsK + (p & 1) * BYTES, ad, h, q, splat16(0.f)); };
   auto next = [&](int p) {
     tile_barrier();
     if (p + 2 < order.total) issue_k(p + 2);
@@ -245,8 +245,8 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) * 
   const char *Kt = ldsK + w * FT::BYTES, *Vt = ldsV + w * FT::BYTES;
   const uint32_t atK = lds_at(ldsK) + w * FT::BYTES, atV = lds_at(ldsV) + w * FT::BYTES;
 
-  uint4 q[RT::NS];
-  load_column<T, D>(q, a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
+  Column<T, D> q;
+  q.load(a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
   const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
   // keys in [lo1, hi0) are seen by every query
   const int lo1 = first_key(a, x, b1), hi0 = end_key(a, x, b0);
@@ -265,7 +265,7 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) * 
     const int k0 = kbeg + 32 * t, k1 = k0 + 32 * FT::NW;
     const bool more = t + FT::NW < t1;
     wait_copies<FT::NI>();  // K is here, V may be in flight
-    f32x16 sc = tile_rows<T, D>(Kt, ad, 0, q, splat16(0.f));
+    f32x16 sc = tile_rows<D>(Kt, ad, 0, q, splat16(0.f));
     wait_lds();  // and has been read
     if (more) few_copy<T, D>(atK, kb, k1, a.k.n, x.klen - k1);
     if (!(k0 >= lo1 && k0 + 32 <= hi0)) dense_mask(sc, lo - k0, hi - k0);
