@@ -37,7 +37,7 @@ template <typename T, int D> struct RowTile {
   static constexpr int RB = D * (int)sizeof(T);  // bytes per row
   static constexpr int CPR = RB / 16;            // 16-byte chunks per row
   static constexpr int RPI = 64 / CPR;           // rows one wave-wide copy fills
-  static constexpr int NS = CPR / 2;             // reduction steps of a `rows` product
+  static constexpr int NS = CPR / 2;             // pairs of chunks, one per lane group
   static constexpr int NB = D / 32;              // 32-wide blocks of d
   static constexpr int TR = sizeof(T) == 2 ? 64 : 32;  // rows per staged tile
   // Slot s of row r holds chunk s ^ swz(r). LDS serves 256 bytes per cycle: 16

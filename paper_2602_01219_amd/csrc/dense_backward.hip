@@ -5,7 +5,12 @@
 // Two passes form P and dP each, so that every sum has one owner and no atomics:
 // the query side (32 rows per wave, over the keys) sums dQ, the key side (32 keys
 // per wave, over the rows of all query heads of the key head) sums dK and dV.
-// That is 14 D flops per pair where 10 D would do with dQ added atomically.
+// That is 14 D flops per pair where 10 D would do with dQ added atomically. Both are
+// bound by the MFMAs: 24 heads of 16384 tokens, d = 64, take 2.2 ms (query side)
+// and 3.1 ms (key side), 1.1 PFLOP/s of the products formed; 16 heads of 8192, d =
+// 128, 1.7 ms in all. Where registers are short (the key side at d = 128 holds 192
+// of them in operands and sums) addresses are formed again rather than spilled: a
+// spilled one's load waits for the tile copies in flight (1968 against 1707 us).
 #include "dense.hpp"
 #include "kernels.hpp"
 #include "layer_check.hpp"

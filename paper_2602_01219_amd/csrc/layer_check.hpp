@@ -180,9 +180,8 @@ inline int check_dense(const mita_dense_cfg_t *c, std::string *err) {
 }
 
 // The window as the kernels use it: bounds past every key mean none.
-inline int window(int w, const mita_dense_cfg_t &c) {
+inline int window(int w) {
   const int none = 4 * MITA_DENSE_MAX_N;
-  (void)c;
   return w < 0 || w > none ? none : w;
 }
 
@@ -203,7 +202,7 @@ inline int keys_seen(const mita_dense_cfg_t &c) {  // most keys one row tile rea
 }
 // `uneven`: the window gives workgroups different lengths, which even out over two
 // rounds of them (16 heads of 4 key heads, 8192 tokens, causal, d = 128, backward:
-// 1718 us with one round).
+// 1718 us in one round, 1126 in two).
 inline int splits_for(int64_t blocks, int64_t len, int64_t least, bool uneven) {
   // (rounded down: 960 workgroups of a causal forward, 5 sequences of 2039 tokens,
   // d = 128, take 62 us whole and 103 split in two, by the partial results)
@@ -220,8 +219,8 @@ inline DensePlan dense_plan(const mita_dense_cfg_t &c) {
     return p;
   }
   p.tiles = (int)((dense_rows(c) + DENSE_FEW - 1) / DENSE_FEW);
-  // just over two workgroups per CU (192 slices of up to 16384 keys, d = 128: 217 us;
-  // one per CU 234, four 229, eight 242, as every workgroup starts with nothing in
+  // just over two workgroups per CU (192 slices of up to 16384 keys, d = 128: 208 us;
+  // one per CU 228, four 212, eight 218, as every workgroup starts with nothing in
   // flight), 256 keys each at least (1024 of more rows, whose join takes 4 us)
   const int64_t blocks = slices(c) * p.tiles, want = (2 * CUS) / blocks + (dense_rows(c) <= DENSE_FEW ? 1 : 0);
   const int64_t least = dense_rows(c) <= DENSE_FEW ? 256 : 1024;
@@ -236,9 +235,9 @@ struct DenseBwdPlan {
 };
 inline DenseBwdPlan dense_bwd_plan(const mita_dense_cfg_t &c) {
   DenseBwdPlan p;
-  // the shortest piece (an fp32 step takes eight times a bf16 one's MFMA time): 8
+  // the shortest piece (an fp32 step takes six times a bf16 one's MFMA time): 8
   // causal heads of 1000 bf16 tokens, d = 64, take 38 us at 256, 40 at 128, 48 at
-  // 512; 8 heads of 500 fp32 tokens 50 us at 64, 66 at 128, 59 at 32
+  // 512; 8 heads of 500 fp32 tokens 50 us at 64, 60 at 128, 114 at 256, 58 at 32
   const int64_t least = c.dtype == MITA_F32 ? 64 : 256;
   p.qtiles = (int)((dense_rows(c) + DENSE_TQ - 1) / DENSE_TQ);
   p.qsplits = splits_for(slices(c) * p.qtiles, keys_seen(c), least, uneven(c));

@@ -3,12 +3,17 @@
 // Forward: y = (x - mean) rstd w + b. Backward, with h = (x - mean) rstd and
 // g = dy w: dx = rstd (g - mean(g) - h mean(g h)), dw = sum dy h, db = sum dy.
 // Both are bound by HBM: a row is read once into registers, its sums go across
-// the lanes that share it, and it is written once; the next row's loads are
-// issued before the current row is reduced. The variance is summed about the
-// mean from the registers (a one-pass sum of squares cancels where the mean is
-// large). In the backward each lane keeps the sums of dw and db of its own
-// columns over all rows its workgroup takes; one partial sum per workgroup goes
-// to memory, and a second launch adds them in a fixed order.
+// the lanes that share it (DPP within a wave), and it is written once. The variance
+// is summed about the mean from the registers (a one-pass sum of squares cancels
+// where the mean is large). Loads and stores share one counter, so a loop that
+// fetches the next row early waits for the stores of the last: rows come in waves
+// that end instead (forward) or enough waves (backward). In the backward each lane
+// keeps the sums of dw and db of its own columns over all rows its workgroup takes;
+// one partial sum per workgroup goes to memory, and a second launch adds them in a
+// fixed order. Measured: queries of 2 x 12 heads x 16384 tokens, d = 64, bf16, 19.9 us
+// (104 MB: 5.3 TB/s; 26.0 as a persistent loop); backward of 32768 x 768 bf16
+// 30 us and 4 for the sums (151 MB, 5 TB/s in the first; 37 as a loop that
+// prefetched).
 #include "cdna4.hpp"
 #include "kernels.hpp"
 #include "layer_check.hpp"
