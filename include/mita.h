@@ -351,7 +351,8 @@ typedef struct {
  */
 typedef struct {
   int32_t B, H, H_kv;      /* batch, query heads (at most 4096), key/value heads; H_kv divides H; N * H / H_kv
-                              at most 2^27 (MITA_ERR_UNSUPPORTED beyond) */
+                              at most 2^27, and B * H_kv pieces of 32 such rows, or of 32 keys, fewer than
+                              2^24 (MITA_ERR_UNSUPPORTED beyond) */
   int32_t N, N_k, d;       /* queries, keys (each in [1, MITA_DENSE_MAX_N]), head dim in {64, 128} */
   int32_t dtype;           /* MITA_F32 or MITA_BF16: storage of all tensors but the log-sum-exps */
   int32_t left, right;     /* window, -1 for no bound */
@@ -408,6 +409,8 @@ int mita_dense_backward(const mita_dense_cfg_t *cfg, const void *q, const void *
 
 /* Widest row of the layer norm. */
 #define MITA_NORM_MAX_C 65536
+/* Most rows of the layer norm. */
+#define MITA_NORM_MAX_ROWS (1 << 30)
 
 /*
  * Layer norm over the C elements of each row of an [n[0], n[1], n[2], C]
@@ -417,7 +420,7 @@ int mita_dense_backward(const mita_dense_cfg_t *cfg, const void *q, const void *
  * and widths are multiples of 16 bytes are read and written 16 bytes at a time.
  */
 typedef struct {
-  int32_t n[3], C;         /* rows, 1 <= C <= MITA_NORM_MAX_C */
+  int32_t n[3], C;         /* rows (n[0] n[1] n[2] <= MITA_NORM_MAX_ROWS), 1 <= C <= MITA_NORM_MAX_C */
   int32_t dtype;           /* MITA_F32 or MITA_BF16: x, y, dy, dx */
   int32_t wdtype;          /* MITA_F32 or MITA_BF16: w, b, dw, db */
   float eps;               /* > 0 */

@@ -152,7 +152,8 @@ inline int check_dense(const mita_dense_cfg_t *c, std::string *err) {
   if (c->H > 4096) return fail(MITA_ERR_UNSUPPORTED, "H must not exceed 4096");
   // row numbers are 32-bit, and so are the grids
   if (dense_rows(*c) > (1 << 27)) return fail(MITA_ERR_UNSUPPORTED, "N * (H / H_kv) must not exceed 2^27");
-  if (slices(*c) * ((dense_rows(*c) + 31) / 32) > (1 << 25) || slices(*c) * ((c->N_k + 31) / 32) > (1 << 25))
+  // (workgroups of 256 threads, of which a launch has less than 2^32)
+  if (slices(*c) * ((dense_rows(*c) + 31) / 32) >= (1 << 24) || slices(*c) * ((c->N_k + 31) / 32) >= (1 << 24))
     return fail(MITA_ERR_UNSUPPORTED, "too many heads and tokens for one launch");
   const int64_t unit = 16 / (int64_t)elem_bytes(*c);
   const struct {
@@ -325,8 +326,9 @@ inline int check_norm(const mita_norm_cfg_t *c, std::string *err) {
       return fail(MITA_ERR_UNSUPPORTED, "dtype and wdtype must be MITA_F32 or MITA_BF16");
   if (c->C > MITA_NORM_MAX_C) return fail(MITA_ERR_UNSUPPORTED, "C must not exceed MITA_NORM_MAX_C");
   if (!(c->eps > 0.f) || std::isinf(c->eps)) return fail(MITA_ERR_INVALID_ARG, "eps must be finite and > 0");
-  if ((int64_t)c->n[0] * c->n[1] > INT32_MAX || norm_rows(*c) > INT32_MAX)
-    return fail(MITA_ERR_UNSUPPORTED, "too many rows");
+  // row numbers are 32-bit, with room for a workgroup past the last
+  if ((int64_t)c->n[0] * c->n[1] > MITA_NORM_MAX_ROWS || norm_rows(*c) > MITA_NORM_MAX_ROWS)
+    return fail(MITA_ERR_UNSUPPORTED, "more than MITA_NORM_MAX_ROWS rows");
   const struct {
     const char *name;
     const int64_t (&s)[3];

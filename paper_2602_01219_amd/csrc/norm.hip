@@ -193,6 +193,11 @@ template <int TPR, int THREADS, int K> struct RowSum {
 // does not go on to others: nothing would wait for its stores, but the next loads
 // would (loads and stores share one counter).
 template <int TPR> constexpr int fwd_threads = TPR > NORM_FWD_THREADS ? TPR : NORM_FWD_THREADS;
+// Workgroups along x: a dimension of a launch has less than 2^32 threads.
+constexpr int NORM_GRID_X = 1 << 21;
+inline dim3 norm_grid(int blocks) {
+  return dim3((unsigned)std::min(blocks, NORM_GRID_X), (unsigned)((blocks + NORM_GRID_X - 1) / NORM_GRID_X));
+}
 template <int TPR> constexpr int bwd_threads = TPR > NORM_BWD_THREADS ? TPR : NORM_BWD_THREADS;
 template <typename T, int VE, int TPR, int P, int U>
 __global__ void __launch_bounds__(fwd_threads<TPR>) norm_fwd_kernel(NormArgs a) {
@@ -200,7 +205,8 @@ __global__ void __launch_bounds__(fwd_threads<TPR>) norm_fwd_kernel(NormArgs a) 
   constexpr int RPB = Sum::ROWS;
   __shared__ float red[2][Sum::ROWS][Sum::W][1];
   Sum row_sum{red};
-  const int t = threadIdx.x % TPR, r0 = blockIdx.x * RPB * U + threadIdx.x / TPR;
+  const int block = blockIdx.y * NORM_GRID_X + blockIdx.x;
+  const int t = threadIdx.x % TPR, r0 = block * RPB * U + threadIdx.x / TPR;
   RowRegs<T, VE, TPR, P> x[U];
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -492,9 +498,9 @@ template <typename T, int VE, int TPR, int P> hipError_t fwd_p(const NormArgs &a
   // as many rows per thread as give four pieces, once that leaves eight workgroups per CU
   constexpr int N = fwd_threads<TPR>, RPB = N / TPR, U = P >= 4 ? 1 : P >= 2 ? 2 : 4;
   if (U > 1 && a.rows >= RPB * U * 8 * CUS)
-    norm_fwd_kernel<T, VE, TPR, P, U><<<dim3((unsigned)((a.rows + RPB * U - 1) / (RPB * U))), N, 0, st>>>(a);
+    norm_fwd_kernel<T, VE, TPR, P, U><<<norm_grid((a.rows + RPB * U - 1) / (RPB * U)), N, 0, st>>>(a);
   else
-    norm_fwd_kernel<T, VE, TPR, P, 1><<<dim3((unsigned)((a.rows + RPB - 1) / RPB)), N, 0, st>>>(a);
+    norm_fwd_kernel<T, VE, TPR, P, 1><<<norm_grid((a.rows + RPB - 1) / RPB), N, 0, st>>>(a);
   return launched("norm_fwd_kernel", st);
 }
 template <typename T, int VE, int TPR, int P> hipError_t bwd_p(const NormArgs &a, int blocks, hipStream_t st) {

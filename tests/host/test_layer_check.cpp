@@ -57,6 +57,8 @@ int main() {
       {[](mita_dense_cfg_t &x) { x.v = {51200, 64, (int64_t)MITA_DENSE_MAX_STRIDE + 8}; }, MITA_ERR_INVALID_ARG},
       {[](mita_dense_cfg_t &x) { x.H = 8192; x.H_kv = 8192; }, MITA_ERR_UNSUPPORTED},
       {[](mita_dense_cfg_t &x) { x.H = 4096; x.H_kv = 1; x.N = 65536; }, MITA_ERR_UNSUPPORTED},
+      {[](mita_dense_cfg_t &x) { x.B = 1 << 20; }, MITA_ERR_UNSUPPORTED},                // 2^21 x 13 pieces of 32 rows
+      {[](mita_dense_cfg_t &x) { x.B = 1 << 23, x.N = x.N_k = 1; }, MITA_ERR_UNSUPPORTED},  // 2^24
   };
   for (const Bad &b : bad) {
     mita_dense_cfg_t x = c;

@@ -143,6 +143,35 @@ def test_without_weights_and_far_from_zero():
     assert float((rstd.double() * cfg.eps ** 0.5 - 1).abs().max()) <= 4 * U
 
 
+def test_more_rows_than_one_grid_dimension():
+    """2^27 + 5 rows of 9, a wave each, two rows per wave: 2^32 threads and more."""
+    g = gen(12)
+    R, C = 2 ** 27 + 5, 9
+    cfg = mita.NormConfig((R,), C)
+    x = torch.randn((R, C), device="cuda", generator=g, dtype=torch.bfloat16)
+    y = torch.full_like(x, float("nan"))
+    y, mu, rs = mita.norm_forward(cfg, x, y=y)
+    dx, _, _ = mita.norm_backward(cfg, x, mu, rs, x, dx=torch.full_like(x, float("nan")), want_weights=False)
+    # workgroup 2^21, the first of the second row of the grid, takes row 2^24
+    for at in (0, 2 ** 24 - 500, 2 ** 26, R - 1000):
+        X = x[at:at + 1000].to(F64)
+        c = X - X.mean(-1, keepdim=True)
+        var = (c * c).mean(-1, keepdim=True) + cfg.eps
+        Y = c * var ** -0.5
+        # |x| < 6 and 9 elements: fp32 mean and x - mean are off by 11 U 6 + 6 U < 5e-6; with that, rstd by
+        # 5e-6 rstd of itself, so y by 5e-6 rstd (1 + |y|), |y| < 3, and by the rounding of bf16; twice all of it
+        err = 2 * (5e-6 * var ** -0.5 * 4 + half_step("bf16") * Y.abs())
+        assert worst(y[at:at + 1000], Y, err) <= 1.0
+        G = (X * Y).mean(-1, keepdim=True)
+        D = var ** -0.5 * (c - Y * G)
+        # dy = x: c, Y and G (|G| = |mean(x y)| < 6) each carry the errors above
+        ed = 2 * (var ** -0.5 * (5e-6 + 5e-6 * var ** -0.5 * 4 * (6 + 2 * Y.abs() * 6)
+                                 + 5e-6 * var ** -0.5 * (c.abs() + (Y * G).abs()) + 12 * U * (c.abs() + 6 * Y.abs()))
+                  + half_step("bf16") * D.abs())
+        assert worst(dx[at:at + 1000], D, ed) <= 1.0
+    assert all(bool(torch.isfinite(t).all()) for t in (y, mu, rs, dx))
+
+
 def test_one_dimensional_rows_in_place_and_parts():
     cfg = mita.NormConfig((300,), 384, dtype="bf16")
     g = gen(5)

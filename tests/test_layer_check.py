@@ -91,3 +91,18 @@ def test_norm_refusals():
     assert bwd(ws=None) == mita.MITA_ERR_WORKSPACE and bwd(n=8) == mita.MITA_ERR_WORKSPACE
     with pytest.raises(ValueError):
         mita.NormConfig((1, 2, 3, 4), 64).struct()
+
+
+@needs_lib
+def test_sizes_past_a_launch():
+    lib = mita.load_library()
+    # workgroups of 256 threads, one per 32 rows (or keys) of a slice, of which a launch has less than 2^32 / 256
+    assert mita.dense_check(mita.DenseConfig(2 ** 21, 4, 32, 64)) == mita.MITA_OK
+    assert mita.dense_check(mita.DenseConfig(2 ** 21, 8, 32, 64)) == mita.MITA_ERR_UNSUPPORTED
+    assert mita.dense_check(mita.DenseConfig(2 ** 20, 8, 1, 64, N_k=64)) == mita.MITA_ERR_UNSUPPORTED
+    for rows in ((2 ** 30 + 1,), (2 ** 15, 2 ** 15, 2)):
+        cfg = mita.NormConfig(rows, 9)
+        assert mita.norm_check(cfg) == mita.MITA_ERR_UNSUPPORTED
+        assert lib.mita_norm_forward(ctypes.byref(cfg.struct()), A[0], None, None, A[0], None, None,
+                                     None) == mita.MITA_ERR_UNSUPPORTED
+    assert mita.norm_check(mita.NormConfig((2 ** 30,), 9)) == mita.MITA_OK
