@@ -331,6 +331,8 @@ int mita_backward(const mita_cfg_t *cfg, const void *q, const void *k, const voi
 
 /* Longest query or key sequence of the dense attention. */
 #define MITA_DENSE_MAX_N (1 << 20)
+/* Largest score scale q_i . k_j of the dense attention (2^27 log 2). */
+#define MITA_DENSE_MAX_SCORE 9.3e7f
 /* Largest distance between two tokens of one head, in elements. */
 #define MITA_DENSE_MAX_STRIDE (1 << 22)
 
@@ -381,7 +383,11 @@ size_t mita_dense_workspace_size(const mita_dense_cfg_t *cfg, int which);
  *   ws   : >= mita_dense_workspace_size(cfg, MITA_WS_FORWARD) bytes.
  * A query that sees no key, and every query behind its sequence's end, gets
  * o = 0 and lse = -infinity. Values a window hides must be finite (NaN or
- * infinite inputs inside a sequence are a caller error, as everywhere).
+ * infinite inputs inside a sequence are a caller error, as everywhere). Scores
+ * are supported up to MITA_DENSE_MAX_SCORE in size: a query that sees a larger
+ * one, or one that is NaN, gets o and lse NaN (and NaN gradients); scores below
+ * -MITA_DENSE_MAX_SCORE have no weight, and a query that sees nothing else is
+ * NaN too.
  * Scores, softmax and sums are fp32; in bf16 the weights are rounded once to
  * bf16 to multiply v. Results are the same bit for bit from call to call.
  * A few queries against many keys (single tokens) are split over the keys.

@@ -37,6 +37,11 @@ __device__ __forceinline__ void dense_mask(f32x16 &s, int lo, int hi) {
 
 // The reference moves only where a score passes it by more than RESCALE_LOG2 (and
 // at the column's first visible key): any reference gives the same softmax.
+// Near DENSE_MAX_LOG2 = 2^27 fp32 numbers are 8 or 16 apart: z - m of the largest
+// score is up to 4 off 0, and thr up to 24 + 4 off its place, so that weights reach
+// 2^40 at most and their sums stay finite. A larger score makes its row NaN; scores
+// below -2^27 weigh nothing, and a row with no others is 0 / 0.
+constexpr float DENSE_MAX_LOG2 = 134217728.f;
 template <int D> __device__ __forceinline__ void dense_reference(DenseState<D> &st, const f32x16 &s, float sl2) {
   float mx = s[0];
 #pragma unroll
@@ -44,7 +49,8 @@ template <int D> __device__ __forceinline__ void dense_reference(DenseState<D> &
   if (__ballot(mx > st.thr)) {
     const float cm = column_max(mx);
     const bool up = cm > st.thr;
-    const float m = up ? cm * sl2 : -st.nm;
+    const float top = cm * sl2;
+    const float m = !up ? -st.nm : top > DENSE_MAX_LOG2 ? NAN : fmaxf(top, -DENSE_MAX_LOG2);
     const float alpha = st.thr == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-st.nm - m);
     st.nm = -m;
     st.thr = up ? (m + RESCALE_LOG2) * __builtin_amdgcn_rcpf(sl2) : st.thr;
@@ -69,17 +75,27 @@ __device__ __forceinline__ ColsOperand<T> dense_weights(DenseState<D> &st, f32x1
   return ColsOperand<T>(s);
 }
 
+// 1 / l of a row's weight sum l, and its log-sum-exp for the reference m (log2
+// units). `none`: the row has no keys here, 0 and -infinity. A row that has keys but
+// no weight, or weights that are NaN, is NaN.
+__device__ __forceinline__ void dense_norm(bool none, float l, float m, float &inv, float &lse2) {
+  inv = none ? 0.f : 1.f / l;
+  lse2 = none ? -INFINITY : l == 0.f ? NAN : __builtin_amdgcn_logf(l) + m;
+}
+
 // A column's result (weight sum l, reference m in log2 units) to o and lse, or to
-// its split's place. Rows that see nothing: 0 and -infinity.
+// its split's place. `sees`: the row sees keys (some of them, with splits, in other
+// splits: a sum of 0 is one of no keys then).
 template <typename T, int D>
 __device__ __forceinline__ void dense_write(const DenseArgs &a, const DenseSlice &x, int s, int sp, int row, int tok,
-                                            int head, bool exists, bool valid, float l, float m, f32x16 (&o)[D / 32]) {
-  const bool some = valid && l > 0.f;
-  if (!some) {
+                                            int head, bool exists, bool sees, float l, float m, f32x16 (&o)[D / 32]) {
+  const bool none = !sees || (a.splits > 1 && l == 0.f);
+  if (none) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) o[i] = splat16(0.f);
   }
-  const float inv = some ? 1.f / l : 0.f, lse2 = some ? __builtin_amdgcn_logf(l) + m : -INFINITY;
+  float inv, lse2;
+  dense_norm(none, l, m, inv, lse2);
   const bool first = exists && (threadIdx.x & 63) < 32;
   if (a.splits == 1) {
     store_column<D>((T *)(a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n), o, inv, exists);
@@ -149,6 +165,7 @@ __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_fwd_k
   Column<T, D> q;
   q.load(a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
   const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
+  const bool sees = lo < hi;
   // keys that some row of the wave sees (none: the wave only copies)
   const int wr = tile * DENSE_TQ + 32 * w;
   const int w0 = wr < a.R ? div_group(a, wr) : x.qlen, w1 = min(div_group(a, min(wr + 32, a.R) - 1), x.qlen - 1);
@@ -197,7 +214,7 @@ __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_fwd_k
       for (int p = 0; p < order.total; ++p) next(p);
     }
   }
-  dense_write<T, D>(a, x, s, sp, row, tok, head, exists, valid, column_sum(st.l), -st.nm, st.o);
+  dense_write<T, D>(a, x, s, sp, row, tok, head, exists, sees, column_sum(st.l), -st.nm, st.o);
 }
 
 // Few rows (single tokens, small problems): the four waves of a workgroup share 32
@@ -228,7 +245,9 @@ __device__ __forceinline__ void few_copy(uint32_t tile, const char *base, int fi
   }
 }
 
-template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) * D <= 256 ? 2 : 1) dense_few_kernel(DenseArgs a) {
+// (bf16 at d = 64: four workgroups fit a CU's LDS, and 128 registers suffice)
+template <typename T, int D>
+__global__ void __launch_bounds__(256, sizeof(T) * D == 128 ? 4 : sizeof(T) * D == 256 ? 2 : 1) dense_few_kernel(DenseArgs a) {
   using RT = RowTile<T, D>;
   using FT = FewTile<T, D>;
   __shared__ __align__(16) char ldsK[FT::NW * FT::BYTES];
@@ -257,6 +276,7 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) * 
   Column<T, D> q;
   q.load(a.q.p + x.b * a.q.b + head * a.q.h + (int64_t)tok * a.q.n, valid);
   const int lo = valid ? first_key(a, x, tok) : 0, hi = valid ? end_key(a, x, tok) : 0;
+  const bool sees = lo < hi;
   // keys in [lo1, hi0) are seen by every query
   const int lo1 = first_key(a, x, b1), hi0 = end_key(a, x, b0);
   TileAddr<T, D> ad;
@@ -290,14 +310,15 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) * 
   }
 
   // every wave's sums relative to the common maximum, added in pairs: waves 0 and
-  // 2, 1 and 3, then both (element e of a lane's accumulators at 64 e + lane)
+  // 2, 1 and 3, then both (element e of a lane's accumulators at 64 e + lane). A wave
+  // without weights adds 0; one whose sum is NaN stays in the sum.
   const float l = column_sum(st.l);
-  if (lane < 32) join_m[w][n] = l > 0.f ? -st.nm : -INFINITY;
+  if (lane < 32) join_m[w][n] = l == 0.f ? -INFINITY : -st.nm;
   __syncthreads();  // (also: every wave is done with its tiles)
   float m = join_m[0][n];
 #pragma unroll
   for (int i = 1; i < FT::NW; ++i) m = fmaxf(m, join_m[i][n]);
-  const float f = l > 0.f ? __builtin_amdgcn_exp2f(-st.nm - m) : 0.f;
+  const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(-st.nm - m);
   if (lane < 32) join_l[w][n] = l * f;
   float *const jk = (float *)ldsK + lane, *const jv = (float *)ldsV + lane;
   auto each = [&](auto &&op) {
@@ -306,7 +327,7 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) * 
 #pragma unroll
       for (int e = 0; e < 16; ++e) st.o[i][e] = op(st.o[i][e], 16 * i + e);
   };
-  each([&](float o, int) { return f > 0.f ? o * f : 0.f; });
+  each([&](float o, int) { return f == 0.f ? 0.f : o * f; });
   if (w >= 2) each([&](float o, int e) { return jk[((w - 2) * (D / 2) + e) * 64] = o; });
   __syncthreads();
   if (w < 2) each([&](float o, int e) { return o + jk[(w * (D / 2) + e) * 64]; });
@@ -314,8 +335,8 @@ template <typename T, int D> __global__ void __launch_bounds__(256, sizeof(T) * 
   __syncthreads();
   if (w >= 1) return;
   each([&](float o, int e) { return o + jv[e * 64]; });
-  dense_write<T, D>(a, x, s, sp, row, tok, head, exists, valid, (join_l[0][n] + join_l[2][n]) + (join_l[1][n] + join_l[3][n]),
-                    m, st.o);
+  dense_write<T, D>(a, x, s, sp, row, tok, head, exists, sees,
+                    (join_l[0][n] + join_l[2][n]) + (join_l[1][n] + join_l[3][n]), m, st.o);
 }
 
 // Joins a row's splits by their log-sum-exps: D / 4 lanes per row.
@@ -325,7 +346,9 @@ template <typename T, int D> __global__ void __launch_bounds__(256) dense_join_k
   const int c = threadIdx.x % L;
   if (i >= (int64_t)a.B * a.Hkv * a.R) return;
   const int s = (int)(i / a.R), row = (int)(i - (int64_t)s * a.R);
-  const int b = s / a.Hkv, tok = div_group(a, row), head = (s - b * a.Hkv) * a.G + row - tok * a.G;
+  const DenseSlice x = dense_slice(a, s);
+  const int tok = div_group(a, row), head = x.hk * a.G + row - tok * a.G;
+  const bool sees = tok < x.qlen && first_key(a, x, tok) < end_key(a, x, tok);
   float m = -INFINITY;
   for (int j = 0; j < a.splits; ++j) m = fmaxf(m, a.part_lse[i * a.splits + j]);
   float l = 0.f;
@@ -341,14 +364,14 @@ template <typename T, int D> __global__ void __launch_bounds__(256) dense_join_k
     o.z += f * y.z;
     o.w += f * y.w;
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  T *out = (T *)(a.o.p + b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n) + 4 * c;
+  float inv, lse2;
+  dense_norm(!sees, l, m, inv, lse2);
+  T *out = (T *)(a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n) + 4 * c;
   out[0] = from_f32<T>(o.x * inv);
   out[1] = from_f32<T>(o.y * inv);
   out[2] = from_f32<T>(o.z * inv);
   out[3] = from_f32<T>(o.w * inv);
-  if (a.lse && c == 0)
-    a.lse[((int64_t)b * a.H + head) * a.N + tok] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+  if (a.lse && c == 0) a.lse[((int64_t)x.b * a.H + head) * a.N + tok] = lse2 * 0.69314718055994531f;
 }
 
 DenseArgs dense_args(const mita_dense_cfg_t &c) {
