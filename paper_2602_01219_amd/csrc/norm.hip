@@ -283,7 +283,10 @@ __global__ void __launch_bounds__(bwd_threads<TPR>) norm_bwd_kernel(NormArgs a) 
     x.load((const T *)a.x + row_at(a, a.sx, rc), a.C, t);
     y.load((const T *)a.dy + row_at(a, a.sdy, rc), a.C, t);
     const int64_t at = row_at(a, a.stat, rc);
-    const float mean = a.mean_in[at], rstd = a.rstd_in[at], on = r < a.rows ? 1.f : 0.f;
+    const float mean = a.mean_in[at], rstd = a.rstd_in[at];
+    // lanes past the last row hold its dy, or, with dx in dy's place, what its own
+    // lanes have written there by now
+    const bool on = r < a.rows;
     float sm[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < P; ++j) {
@@ -297,8 +300,8 @@ __global__ void __launch_bounds__(bwd_threads<TPR>) norm_bwd_kernel(NormArgs a) 
         sm[0] += gw;
         sm[1] = __builtin_fmaf(gw, h, sm[1]);
         if (WG) {
-          dw[j][e] = __builtin_fmaf(yv[e] * on, h, dw[j][e]);
-          db[j][e] = __builtin_fmaf(yv[e], on, db[j][e]);
+          dw[j][e] = on ? __builtin_fmaf(yv[e], h, dw[j][e]) : dw[j][e];
+          db[j][e] = on ? db[j][e] + yv[e] : db[j][e];
         }
       }
     }
