@@ -13,6 +13,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import math
+import operator
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -424,8 +425,9 @@ class DenseConfig(_Planned):
         return torch.float32 if self.dtype == "f32" else torch.bfloat16
 
     def struct(self, **tensors) -> DenseCfgStruct:
-        c = DenseCfgStruct(self.B, self.H, self.H_kv or self.H, self.N, self.N_k or self.N, self.d,
-                           _dtype_code(self.dtype), self.left, self.right, float(self.scale))
+        B, H, N, d, left, right = (_int32(n, getattr(self, n)) for n in ("B", "H", "N", "d", "left", "right"))
+        c = DenseCfgStruct(B, H, _int32("H_kv", self.H_kv) or H, N, _int32("N_k", self.N_k) or N, d,
+                           _dtype_code(self.dtype), left, right, _fp32("scale", self.scale))
         for name, t in tensors.items():
             setattr(c, name, StridesStruct(*_strides(t)))
         return c
@@ -458,14 +460,30 @@ class NormConfig(_Planned):
             raise ValueError("rows must have one to three dimensions")
         pad = 3 - len(self.rows)
         c = NormCfgStruct()
-        c.n = (ctypes.c_int32 * 3)(*([1] * pad + [int(n) for n in self.rows]))
-        c.C, c.dtype, c.wdtype, c.eps = self.C, _dtype_code(self.dtype), _dtype_code(self.wdtype), float(self.eps)
+        c.n = (ctypes.c_int32 * 3)(*([1] * pad + [_int32("rows", n) for n in self.rows]))
+        c.C, c.eps = _int32("C", self.C), _fp32("eps", self.eps)
+        c.dtype, c.wdtype = _dtype_code(self.dtype), _dtype_code(self.wdtype)
         for name, t in tensors.items():
             s = [0] * pad + _row_strides(t)
             if any(s):
                 # dimensions in front of the rows have one entry: any distance will do
                 setattr(c, name, (ctypes.c_int64 * 3)(*[x or self.C for x in s[:pad]], *s[pad:]))
         return c
+
+
+def _int32(name: str, value) -> int:
+    """The value, if the C struct's field holds it (ctypes would cut it off)."""
+    v = operator.index(value)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{name} = {v} does not fit in 32 bits")
+    return v
+
+
+def _fp32(name: str, value) -> float:
+    v = float(value)
+    if v != 0.0 and ctypes.c_float(v).value == 0.0:
+        raise ValueError(f"{name} = {v} is 0 in fp32")
+    return v
 
 
 def _dtype_code(name: str) -> int:
