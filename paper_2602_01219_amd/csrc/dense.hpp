@@ -13,9 +13,8 @@
 // which rows a group takes is free as long as both operands agree: the
 // accumulator's own rows serve, so P never moves between lanes.
 // bf16: one v_mfma_f32_32x32x16_bf16 per 16-long reduction step. fp32: each operand
-// as three bf16 numbers that add up to it exactly (8 bits of its 24 each), and six
-// of the nine products; the three left out are below 2^-23 of the product, about
-// fp32's own rounding. That takes 6 x 32 cycles of the matrix cores per 16-long step where the
+// as three bf16 numbers that add up to it exactly, and six of the nine products (see
+// Split for the three left out). That takes 6 x 32 cycles of the matrix cores per 16-long step where the
 // fp32 instruction takes 8 x 64, and splitting an operand on the way (44 VALU
 // instructions per 8 elements and lane) runs beside it: 16 heads of 2048 tokens, d =
 // 128, 310 -> 224 us forward and 1049 -> 800 backward, 154 TFLOP/s of fp32 products.
@@ -188,11 +187,23 @@ __device__ __forceinline__ f32x16 mma32(const uint4 &a, const uint4 &b, f32x16 c
                                                  0);
 }
 
-// Eight fp32 values as bf16 numbers h + m + l = x: h and m are the upper halves of x
-// and of x - h (no rounding), and l, what is left, has at most 8 bits.
+// Eight fp32 values as bf16 numbers h + m + l = x. `cut`: h and m are the upper halves
+// of x and of x - h, and l, what is left, has at most 8 bits; all have x's sign. `near`:
+// h and m are x and x - h rounded to nearest (the largest fp32 numbers to the largest
+// bf16 one), so that m and l have either sign; for operands that are split once.
+// The products m l', l m' and l l' are left out. With one operand `near` (a column: rows
+// times columns) they are at most 2^-22.4 of the product, of either sign and 0 on
+// average. With both `cut` (the sums of rows weighted by P or dS, where splitting P
+// `near` for every tile costs 1 to 3% of the call) they are at most 2^-21 and have the
+// product's sign: such a product is low by 2^-24.7 of itself on average, 0.6 of half an
+// fp32 step.
 struct Split {
   uint4 h, m, l;
-  __device__ __forceinline__ void set(const float (&x)[8]) {
+  __device__ __forceinline__ static uint4 upper(const uint32_t (&v)[8]) {
+    return make_uint4(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u),
+                      __builtin_amdgcn_perm(v[5], v[4], 0x07060302u), __builtin_amdgcn_perm(v[7], v[6], 0x07060302u));
+  }
+  __device__ __forceinline__ void cut(const float (&x)[8]) {
     uint32_t u[3][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -201,20 +212,31 @@ struct Split {
       u[1][i] = __float_as_uint(r);
       u[2][i] = __float_as_uint(r - __uint_as_float(u[1][i] & 0xffff0000u));
     }
-    auto upper = [](const uint32_t (&v)[8]) {
-      return make_uint4(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u),
-                        __builtin_amdgcn_perm(v[5], v[4], 0x07060302u), __builtin_amdgcn_perm(v[7], v[6], 0x07060302u));
-    };
     h = upper(u[0]);
     m = upper(u[1]);
     l = upper(u[2]);
   }
-  __device__ __forceinline__ void set(const uint4 &a, const uint4 &b) {
-    const float x[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
-                        __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
-    set(x);
+  __device__ __forceinline__ void near(const float (&x)[8]) {
+    const float most = __uint_as_float(0x7f7f0000u);
+    uint32_t a[4], b[4], c[8];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      a[i / 2] = pack_bf16x2(__builtin_amdgcn_fmed3f(x[i], -most, most), __builtin_amdgcn_fmed3f(x[i + 1], -most, most));
+      const float r[2] = {x[i] - __uint_as_float(a[i / 2] << 16), x[i + 1] - __uint_as_float(a[i / 2] & 0xffff0000u)};
+      b[i / 2] = pack_bf16x2(r[0], r[1]);
+      c[i] = __float_as_uint(r[0] - __uint_as_float(b[i / 2] << 16));
+      c[i + 1] = __float_as_uint(r[1] - __uint_as_float(b[i / 2] & 0xffff0000u));
+    }
+    h = make_uint4(a[0], a[1], a[2], a[3]);
+    m = make_uint4(b[0], b[1], b[2], b[3]);
+    l = upper(c);
+  }
+  __device__ __forceinline__ static void floats(float (&x)[8], const uint4 &a, const uint4 &b) {
+    x[0] = __uint_as_float(a.x), x[1] = __uint_as_float(a.y), x[2] = __uint_as_float(a.z), x[3] = __uint_as_float(a.w);
+    x[4] = __uint_as_float(b.x), x[5] = __uint_as_float(b.y), x[6] = __uint_as_float(b.z), x[7] = __uint_as_float(b.w);
   }
 };
+// The six products of the largest parts.
 __device__ __forceinline__ f32x16 mma32(const Split &a, const Split &b, f32x16 c) {
   c = mma32(a.l, b.h, c);
   c = mma32(a.h, b.l, c);
@@ -247,7 +269,11 @@ template <int D> struct Column<float, D> {
     for (int s = 0; s < 2 * NS; ++s)
       x[s] = valid ? *reinterpret_cast<const uint4 *>(row + 32 * s + 16 * g) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) b[s].set(x[2 * s], x[2 * s + 1]);
+    for (int s = 0; s < NS; ++s) {
+      float y[8];
+      Split::floats(y, x[2 * s], x[2 * s + 1]);
+      b[s].near(y);
+    }
   }
 };
 // The scalar product of a column's rows x and y (0 without them), in both its lanes' parts.
@@ -283,9 +309,11 @@ __device__ __forceinline__ f32x16 tile_rows(const char *tile, const TileAddr<flo
   using RT = RowTile<float, D>;
 #pragma unroll
   for (int s = 0; s < RT::NS; s += 2) {
+    float x[8];
+    Split::floats(x, *reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)(s << 5)) + kb * 32 * RT::RB),
+                  *reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)((s + 1) << 5)) + kb * 32 * RT::RB));
     Split a;
-    a.set(*reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)(s << 5)) + kb * 32 * RT::RB),
-          *reinterpret_cast<const uint4 *>(tile + (ad.r0 ^ (uint32_t)((s + 1) << 5)) + kb * 32 * RT::RB));
+    a.cut(x);
     c = mma32(a, col.b[s / 2], c);
   }
   return c;
@@ -309,7 +337,7 @@ template <> struct ColsOperand<float> {
     for (int s = 0; s < 2; ++s) {
       const float x[8] = {p[8 * s],     p[8 * s + 1], p[8 * s + 2], p[8 * s + 3],
                           p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
-      b[s].set(x);
+      b[s].cut(x);
     }
   }
 };
@@ -347,7 +375,7 @@ __device__ __forceinline__ void tile_cols(f32x16 (&acc)[D / 32], const char *til
             tile + (ad.c0 ^ (uint32_t)(((q & 1) << 2 | r) << 4) ^ (uint32_t)(db << 7)) + (32 * kb + 8 * q + r) * RT::RB);
       }
       Split a;
-      a.set(x);
+      a.cut(x);
       acc[db] = mma32(a, P.b[s], acc[db]);
     }
 }
