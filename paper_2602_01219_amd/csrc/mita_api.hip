@@ -426,6 +426,13 @@ template <typename F> int guarded(F &&f) {
     return MITA_ERR_HIP;
   }
 }
+template <typename F> size_t guarded_size(F &&f) {
+  try {
+    return f();
+  } catch (...) {
+    return 0;
+  }
+}
 
 }  // namespace
 
@@ -681,7 +688,9 @@ int mita_dense_check(const mita_dense_cfg_t *cfg) {
   });
 }
 
-size_t mita_dense_workspace_size(const mita_dense_cfg_t *cfg, int which) { return dense_workspace_size(cfg, which); }
+size_t mita_dense_workspace_size(const mita_dense_cfg_t *cfg, int which) {
+  return guarded_size([&]() -> size_t { return dense_workspace_size(cfg, which); });
+}
 
 int mita_dense_forward(const mita_dense_cfg_t *cfg, const void *q, const void *k, const void *v, const int32_t *q_len,
                        const int32_t *k_len, void *o, float *lse, void *ws, size_t ws_bytes, mita_stream_t stream) {
@@ -741,7 +750,9 @@ int mita_norm_check(const mita_norm_cfg_t *cfg) {
   });
 }
 
-size_t mita_norm_workspace_size(const mita_norm_cfg_t *cfg) { return norm_workspace_size(cfg); }
+size_t mita_norm_workspace_size(const mita_norm_cfg_t *cfg) {
+  return guarded_size([&]() -> size_t { return norm_workspace_size(cfg); });
+}
 
 int mita_norm_forward(const mita_norm_cfg_t *cfg, const void *x, const void *w, const void *b, void *y, float *mean,
                       float *rstd, mita_stream_t stream) {
