@@ -61,7 +61,7 @@ template <int D> __device__ __forceinline__ void dense_reference(DenseState<D> &
 }
 
 // The weights exp2(s sl2 - m) as they multiply the values; their sum takes them
-// before that rounding (the rounded ones would put the log-sum-exp off by up to
+// before that rounding (the rounded ones would put the log-sum-exp off by about
 // 2^-9 over the root of the number of keys).
 template <typename T, int D>
 __device__ __forceinline__ ColsOperand<T> dense_weights(DenseState<D> &st, f32x16 s, float sl2) {
@@ -83,9 +83,11 @@ __device__ __forceinline__ void dense_norm(bool none, float l, float m, float &i
   lse2 = none ? -INFINITY : l == 0.f ? NAN : __builtin_amdgcn_logf(l) + m;
 }
 
+// The log-sum-exp of a split without weight whose row sees keys, here or elsewhere.
+constexpr float DENSE_NO_WEIGHT = -3.4028235e38f;
+
 // A column's result (weight sum l, reference m in log2 units) to o and lse, or to
-// its split's place. `sees`: the row sees keys (some of them, with splits, in other
-// splits: a sum of 0 is one of no keys then).
+// its split's place. `sees`: the row sees keys.
 template <typename T, int D>
 __device__ __forceinline__ void dense_write(const DenseArgs &a, const DenseSlice &x, int s, int sp, int row, int tok,
                                             int head, bool exists, bool sees, float l, float m, f32x16 (&o)[D / 32]) {
@@ -96,6 +98,7 @@ __device__ __forceinline__ void dense_write(const DenseArgs &a, const DenseSlice
   }
   float inv, lse2;
   dense_norm(none, l, m, inv, lse2);
+  if (none && sees) lse2 = DENSE_NO_WEIGHT;
   const bool first = exists && (threadIdx.x & 63) < 32;
   if (a.splits == 1) {
     store_column<D>((T *)(a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n), o, inv, exists);
@@ -346,16 +349,18 @@ template <typename T, int D> __global__ void __launch_bounds__(256) dense_join_k
   const int c = threadIdx.x % L;
   if (i >= (int64_t)a.B * a.Hkv * a.R) return;
   const int s = (int)(i / a.R), row = (int)(i - (int64_t)s * a.R);
-  const DenseSlice x = dense_slice(a, s);
-  const int tok = div_group(a, row), head = x.hk * a.G + row - tok * a.G;
-  const bool sees = tok < x.qlen && first_key(a, x, tok) < end_key(a, x, tok);
-  float m = -INFINITY;
-  for (int j = 0; j < a.splits; ++j) m = fmaxf(m, a.part_lse[i * a.splits + j]);
-  float l = 0.f;
+  const int b = s / a.Hkv, tok = div_group(a, row), head = (s - b * a.Hkv) * a.G + row - tok * a.G;
+  float m = -INFINITY, l = 0.f;
+  bool sees = false;
+  for (int j = 0; j < a.splits; ++j) {
+    const float z = a.part_lse[i * a.splits + j];
+    sees |= z != -INFINITY;
+    m = fmaxf(m, z);
+  }
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int j = 0; j < a.splits; ++j) {
     const float z = a.part_lse[i * a.splits + j];
-    if (z == -INFINITY) continue;  // no visible key in this split
+    if (z <= DENSE_NO_WEIGHT) continue;
     const float f = __builtin_amdgcn_exp2f(z - m);
     const float4 y = *reinterpret_cast<const float4 *>(a.part_o + (i * a.splits + j) * D + 4 * c);
     l += f;
@@ -366,12 +371,12 @@ template <typename T, int D> __global__ void __launch_bounds__(256) dense_join_k
   }
   float inv, lse2;
   dense_norm(!sees, l, m, inv, lse2);
-  T *out = (T *)(a.o.p + x.b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n) + 4 * c;
+  T *out = (T *)(a.o.p + b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n) + 4 * c;
   out[0] = from_f32<T>(o.x * inv);
   out[1] = from_f32<T>(o.y * inv);
   out[2] = from_f32<T>(o.z * inv);
   out[3] = from_f32<T>(o.w * inv);
-  if (a.lse && c == 0) a.lse[((int64_t)x.b * a.H + head) * a.N + tok] = lse2 * 0.69314718055994531f;
+  if (a.lse && c == 0) a.lse[((int64_t)b * a.H + head) * a.N + tok] = lse2 * 0.69314718055994531f;
 }
 
 DenseArgs dense_args(const mita_dense_cfg_t &c) {
