@@ -399,7 +399,9 @@ int mita_dense_forward(const mita_dense_cfg_t *cfg, const void *q, const void *k
  * Gradients of mita_dense_forward's o for an upstream gradient dO, from its
  * inputs and outputs: P_ij = exp(scale q_i . k_j - lse_i) is formed again,
  * D_i = dO_i . o_i, dS = P (dO v^T - D), dq = scale dS k, dk = scale dS^T q,
- * dv = P^T dO, the key side summed over the query heads of each key head.
+ * dv = P^T dO, the key side summed over the query heads of each key head. All
+ * of it is fp32, but that in bf16 P and dS are rounded once to bf16 to multiply
+ * k, q and dO, as the weights of the forward are.
  *   q, k, v, q_len, k_len : the forward's;  o, lse : its outputs;
  *   dO, dq : [B, H, N, d];  dk, dv : [B, H_kv, N_k, d] by cfg's strides; the
  *          gradients must not overlap the inputs or each other;

@@ -190,6 +190,12 @@ inline int window(int w) {
 // those leave CUs without work, DENSE_FEW rows whose keys its waves share. While
 // workgroups are few (two fit a CU) the keys of each are split, at least 512 keys
 // each; the splits' results are joined by their log-sum-exps.
+// Below 256 tiles of DENSE_TQ rows, bf16, us by DENSE_FEW rows and by DENSE_TQ: d = 64,
+// heads of 1000 tokens: 8 heads 11 and 19, 16 13 and 19, 30 (240 tiles) 19.2 and 20.3; two
+// heads of 8192 59 and 63, of 16256 (254 tiles) 204 and 184. d = 128: 8 heads of 1000 15
+// and 24, 16 20 and 25, 24 (192 tiles) 30 and 26; two heads of 8192 97 and 85, of 16256 366
+// and 281: there, and for few long heads, DENSE_TQ wins from about 128 tiles on, which
+// this rule does not use.
 struct DensePlan {
   bool few;    // DENSE_FEW rows per workgroup
   int tiles;   // row tiles per slice
@@ -346,7 +352,9 @@ inline int check_norm(const mita_norm_cfg_t *c, std::string *err) {
 }
 
 // Geometry of the norm kernels: `tpr` threads take a row, each `p` pieces of `ve`
-// elements; p == 0: rows too wide for registers, read again in each pass.
+// elements; p == 0: rows too wide for registers, read again in each pass. In
+// registers: up to 16384 bf16 and 8192 fp32 elements in pieces of 16 bytes, 16384 in
+// pieces of two elements, 8192 one by one.
 constexpr int NORM_FWD_THREADS = 256, NORM_BWD_THREADS = 512;  // per workgroup, or tpr if that is more
 struct NormPlan {
   int ve, tpr, p;

@@ -3,7 +3,8 @@
 // Forward: y = (x - mean) rstd w + b. Backward, with h = (x - mean) rstd and
 // g = dy w: dx = rstd (g - mean(g) - h mean(g h)), dw = sum dy h, db = sum dy.
 // Both are bound by HBM: a row is read once into registers, its sums go across
-// the lanes that share it (DPP within a wave), and it is written once. The variance
+// the lanes that share it (DPP within a wave), and it is written once (see norm_plan
+// for the widest rows that fit; wider ones are read once per pass). The variance
 // is summed about the mean from the registers (a one-pass sum of squares cancels
 // where the mean is large). Loads and stores share one counter, so a loop that
 // fetches the next row early waits for the stores of the last: rows come in waves
@@ -13,7 +14,11 @@
 // fixed order. Measured: queries of 2 x 12 heads x 16384 tokens, d = 64, bf16, 19.9 us
 // (104 MB: 5.3 TB/s; 26.0 as a persistent loop); backward of 32768 x 768 bf16
 // 30 us and 4 for the sums (151 MB, 5 TB/s in the first; 37 as a loop that
-// prefetched).
+// prefetched). Wide rows are further from it. 2048 rows forward: 8192 elements fp32 22
+// us (22 at 6.2 TB/s) and bf16 15 (11), 16384 bf16 32 (22), 12288 fp32 in three passes 91 (32).
+// Backward: 8192 bf16 38 (16), 16384 bf16 76 (32), 12288 fp32 138 (49): with 1024
+// threads per row there are 128 registers for each, and the kernels that hold dw and db
+// spill 23 (16-byte pieces of bf16) to 75 (two-element pieces) of them.
 #include "cdna4.hpp"
 #include "kernels.hpp"
 #include "layer_check.hpp"
