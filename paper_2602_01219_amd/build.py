@@ -46,8 +46,9 @@ VGPR_FORM = ["-Xarch_device", "-mllvm=-amdgpu-mfma-vgpr-form=1"]
 # whose third operand is not its result's registers reads it while it runs, and
 # nothing holds back an LDS read behind it that writes those registers: the compiler
 # sets no wait for it. Of these three such a read came too late to be seen, whatever
-# was in flight before them (operands in VGPRs and AGPRs, after chains of 0 to 64); the
-# 64 cycles of v_mfma_f32_32x32x2_f32 took the read's value every time. With the forced
+# was in flight before them (operands in VGPRs and AGPRs, after chains of 0 to 64, one
+# and two waves on each SIMD of the card); the 64 cycles of v_mfma_f32_32x32x2_f32 took
+# the read's value every time. With the forced
 # form an fp32 dQ kernel of that instruction (d = 128) had its row sums' last copies
 # overwritten so: dQ off by 12% on four of 32 keys.
 MFMA = {"v_mfma_f32_16x16x4_f32", "v_mfma_f32_16x16x32_bf16", "v_mfma_f32_32x32x16_bf16"}
@@ -96,7 +97,10 @@ def matrix_instructions(path):
 
 
 def check_matrix_instructions(path):
-    other = matrix_instructions(path) - MFMA
+    names = matrix_instructions(path)
+    if not names:
+        raise RuntimeError(f"no {ARCH} matrix instructions found in {path}")
+    other = names - MFMA
     if other:
         raise RuntimeError(f"{path} holds matrix instructions whose operands were not checked (MFMA): {sorted(other)}")
 

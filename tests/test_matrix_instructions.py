@@ -32,3 +32,10 @@ __global__ void k(const float *x, f32x16 *y) {
     assert build.matrix_instructions(str(obj)) == {"v_mfma_f32_32x32x2_f32"}
     with pytest.raises(RuntimeError, match="32x32x2_f32"):
         build.check_matrix_instructions(str(obj))
+
+
+def test_a_library_without_device_code_is_refused(tmp_path):
+    empty = tmp_path / "empty.so"
+    empty.write_bytes(b"no code objects")
+    with pytest.raises(RuntimeError, match="no gfx950"):
+        build.check_matrix_instructions(str(empty))
