@@ -115,3 +115,26 @@ def test_large_scores_that_are_supported(plan, sign):
     assert float((o - v[:, :, :1]).abs().max()) <= 2.0 ** -23 * float(v.abs().max())
     # fp32 numbers of that size (9.7e7 in log2 units) are 8 apart: half of it in each of three roundings
     assert float((lse.double() - sign * 2.0 ** 26).abs().max()) <= 12
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("plan", list(PLANS))
+def test_gradients_beside_scores_of_the_lowest_values(plan, dtype):
+    # keys without weight get no gradient and give none: as if a length had left them out
+    cfg, q, k, v = inputs(plan, 64, dtype)
+    q[..., 0] = 1.0
+    blank = cfg.N_k - cfg.N - 9
+    k[:, :, :blank, 0] = -3e38 if dtype == "f32" else -1e30
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    dO = torch.randn(q.shape, device="cuda", generator=g).to(q.dtype)
+    o, lse = mita.dense_forward(cfg, q, k, v)
+    dq, dk, dv = mita.dense_backward(cfg, q, k, v, o, lse, dO)
+    assert bool((dk[:, :, :blank] == 0).all()) and bool((dv[:, :, :blank] == 0).all())
+    short = mita.DenseConfig(cfg.B, cfg.H, cfg.N, 64, N_k=cfg.N_k - blank, dtype=dtype, right=0)
+    cut = [t[:, :, blank:] for t in (k, v)]
+    want = mita.dense_backward(short, q, *cut, o, lse, dO)
+    # the same terms in sums of another order or split: at most a few hundred of them, fp32, then one rounding
+    for x, y in zip((dq, dk[:, :, blank:], dv[:, :, blank:]), want):
+        bound = 256 * 2.0 ** -24 * float(y.abs().max()) + 2 * (2.0 ** -8 if dtype == "bf16" else 0) * y.abs().double()
+        assert bool(((x.double() - y.double()).abs() <= bound + 1e-30).all())
