@@ -465,6 +465,123 @@ int mita_norm_forward(const mita_norm_cfg_t *cfg, const void *x, const void *w, 
 int mita_norm_backward(const mita_norm_cfg_t *cfg, const void *x, const void *w, const float *mean, const float *rstd,
                        const void *dy, void *dx, void *dw, void *db, void *ws, size_t ws_bytes, mita_stream_t stream);
 
+/* Storage type of the RMS norm's output alone: 8-bit floating point with 4
+ * exponent and 3 mantissa bits, largest value 448, no infinities. */
+#define MITA_E4M3 2
+
+/*
+ * Root-mean-square norm of rows of C elements with the residual's addition, on
+ * an [n[0], n[1], n[2], C] tensor as the layer norm's: h = x + res, y = h rstd w.
+ * All tensors of rows have their own distances between rows, in elements (of y:
+ * of its type); all zero: contiguous. Any element alignment is accepted.
+ */
+typedef struct {
+  int32_t n[3], C;         /* rows (n[0] n[1] n[2] <= MITA_NORM_MAX_ROWS), 1 <= C <= MITA_NORM_MAX_C */
+  int32_t dtype;           /* MITA_F32 or MITA_BF16: x, res, h, dy, dh, dx */
+  int32_t wdtype;          /* MITA_F32 or MITA_BF16: w, dw */
+  int32_t ytype;           /* of y: dtype, or MITA_E4M3 */
+  int32_t group;           /* with MITA_E4M3: 128 columns share a scale (the last ones those that are left), or 0: the row */
+  float eps;               /* > 0 */
+  int64_t x[3], res[3], h[3], y[3], dy[3], dh[3], dx[3];
+} mita_rms_cfg_t;
+
+/* Host-only validation of cfg; a status code. */
+int mita_rms_check(const mita_rms_cfg_t *cfg);
+
+/* Bytes of workspace mita_rms_backward needs when dw is asked for (0 if cfg is
+ * invalid); mita_rms_forward needs none. */
+size_t mita_rms_workspace_size(const mita_rms_cfg_t *cfg);
+
+/*
+ * h = x + res, rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd w per row, in fp32
+ * from the sum before it is rounded to h's type; each output is rounded once.
+ * With ytype MITA_E4M3, y is codes and scales: a group's scale is the largest
+ * |h rstd w| in it (at least 2^-117) / 448, a code h rstd w / scale rounded to
+ * nearest even, and code * scale the value it stands for. Backward, such an output
+ * is differentiated as if it had not been rounded.
+ *   res  : or NULL (0);  w : [C], or NULL (1);
+ *   h    : output, or NULL (without res it is x's values);
+ *   y    : output; scales : with MITA_E4M3 [n0, n1, n2, ceil(C / group)] fp32
+ *          contiguous output (one per row with group 0), else NULL;
+ *   rstd : [n0, n1, n2] fp32 contiguous output for the backward pass, or NULL.
+ * h, and y in dtype, may each be x or res with the same strides (not both the same
+ * one), and must not overlap an input otherwise. Squares are fp32: a row's mean of
+ * squares has to stay finite there.
+ */
+int mita_rms_forward(const mita_rms_cfg_t *cfg, const void *x, const void *res, const void *w, void *h, void *y,
+                     float *scales, float *rstd, mita_stream_t stream);
+
+/*
+ * With u = h rstd and g = dy w: dx = dh + rstd (g - u mean(g u)) per row, the
+ * gradient of x and of res alike, and dw = sum over rows of dy u. The row sums are
+ * added in a fixed order in fp32 (the same bit for bit from call to call) and
+ * rounded once.
+ *   h : the forward's h (x where there was no residual);  w : the forward's, or NULL;
+ *   rstd : the forward's;  dy : gradient of y, in dtype;  dh : gradient of h, or NULL (0);
+ *   dx : output or NULL;  dw : [C] output or NULL. dx may be dy or dh with the same
+ *   strides, and must not overlap an input otherwise;
+ *   ws : >= mita_rms_workspace_size(cfg) bytes if dw is given.
+ */
+int mita_rms_backward(const mita_rms_cfg_t *cfg, const void *h, const void *w, const float *rstd, const void *dy,
+                      const void *dh, void *dx, void *dw, void *ws, size_t ws_bytes, mita_stream_t stream);
+
+/* Widest head of the rotary positions. */
+#define MITA_ROPE_MAX_D 256
+/* How the angles are scaled (mita_rope_cfg_t.scaling). */
+#define MITA_ROPE_NONE 0
+#define MITA_ROPE_LINEAR 1
+#define MITA_ROPE_BASE 2
+#define MITA_ROPE_PARTS 3
+
+/*
+ * Rotary positions of queries [B, H, N, d] and keys [B, H_kv, N, d]: of the
+ * first rot elements of each head, pair i (elements i and i + rot / 2, or 2 i and
+ * 2 i + 1 if interleaved) turns by the angle pos f_i, f_i = base^(-2 i / rot),
+ * and is multiplied by scale; the other elements stay as they are.
+ * For contexts longer than the trained one:
+ *   MITA_ROPE_LINEAR  f_i / factor;
+ *   MITA_ROPE_BASE    base factor^(rot / (rot - 2)) in base's place, which leaves
+ *                     the first pair and divides the last one's f by factor (rot > 2);
+ *   MITA_ROPE_PARTS   by the turns t a pair makes over `trained` positions: f_i
+ *                     where t >= fast, f_i / factor where t <= slow, between them
+ *                     c f_i + (1 - c) f_i / factor with c = (t - slow) / (fast - slow).
+ * Angles are formed and reduced in 64 bits, so far positions lose nothing; sines,
+ * cosines and products are fp32, each output is rounded once.
+ */
+typedef struct {
+  int32_t B, H, H_kv, N;   /* H_kv: key heads (no relation to H is needed); H, H_kv at most 4096 */
+  int32_t d, rot;          /* head dim in [2, MITA_ROPE_MAX_D], B N d at most 2^32 - 512; rot even in [2, d] */
+  int32_t dtype;           /* MITA_F32 or MITA_BF16 */
+  int32_t interleaved;
+  int32_t scaling;         /* MITA_ROPE_* */
+  int32_t trained;         /* MITA_ROPE_PARTS: positions of training, >= 1 */
+  double base, factor;     /* > 1; >= 1 (factor is not read with MITA_ROPE_NONE) */
+  double slow, fast;       /* MITA_ROPE_PARTS: 0 <= slow < fast */
+  float scale;             /* of the rotated elements; 0 means 1 */
+  int32_t pos_b;           /* distance between the batch elements' positions: N, or 0 for the same positions */
+  int64_t first;           /* without positions: of token 0, |first| <= 2^31 */
+  mita_strides_t q, k;     /* of the inputs; any multiple of an element, tokens too may repeat (distance 0) */
+  mita_strides_t qo, ko;   /* of the outputs */
+} mita_rope_cfg_t;
+
+/* Host-only validation of cfg; a status code. */
+int mita_rope_check(const mita_rope_cfg_t *cfg);
+
+/*
+ * qo, ko = the rotated q, k. k and ko may be NULL (queries alone).
+ *   pos : [N] (pos_b 0) or [B, N] (pos_b N) int32 positions, or NULL: first, first + 1, ..
+ * qo may be q, and ko k, with the same strides; otherwise no output may overlap an
+ * input.
+ */
+int mita_rope_forward(const mita_rope_cfg_t *cfg, const void *q, const void *k, const int32_t *pos, void *qo, void *ko,
+                      mita_stream_t stream);
+
+/* Gradients of mita_rope_forward's inputs from those of its outputs (cfg's q, k
+ * are the strides of dqo, dko, its qo, ko those of dq, dk): the pairs turn back,
+ * times scale. */
+int mita_rope_backward(const mita_rope_cfg_t *cfg, const void *dqo, const void *dko, const int32_t *pos, void *dq,
+                       void *dk, mita_stream_t stream);
+
 /*
  * Per-launch timing of mita_forward with HIP events (profiling aid).
  * A timer holds event slots for up to max_calls forward calls. Each

@@ -219,4 +219,14 @@ hipError_t launch_norm_backward(const mita_norm_cfg_t &c, const void *x, const v
                                 const float *rstd, const void *dy, void *dx, void *dw, void *db, void *ws,
                                 hipStream_t st);
 
+// RMS norm of rows and its gradients (mita_rms_forward, mita_rms_backward).
+hipError_t launch_rms_forward(const mita_rms_cfg_t &c, const void *x, const void *res, const void *w, void *h, void *y,
+                              float *scales, float *rstd, hipStream_t st);
+hipError_t launch_rms_backward(const mita_rms_cfg_t &c, const void *h, const void *w, const float *rstd, const void *dy,
+                               const void *dh, void *dx, void *dw, void *ws, hipStream_t st);
+
+// Rotary positions; `back`: the other way round (mita_rope_forward, mita_rope_backward).
+hipError_t launch_rope(const mita_rope_cfg_t &c, const void *q, const void *k, const int32_t *pos, void *qo, void *ko,
+                       bool back, hipStream_t st);
+
 }  // namespace mita

@@ -306,7 +306,7 @@ inline size_t dense_workspace_size(const mita_dense_cfg_t *c, int which) {
 // ---------------------------------------------------------------------------
 inline size_t elem_bytes(const mita_norm_cfg_t &c) { return c.dtype == MITA_F32 ? 4 : 2; }
 inline int64_t norm_rows(const mita_norm_cfg_t &c) { return (int64_t)c.n[0] * c.n[1] * c.n[2]; }
-inline Strided strided_rows(const mita_norm_cfg_t &c, const int64_t (&s)[3]) {
+template <typename Cfg> Strided strided_rows(const Cfg &c, const int64_t (&s)[3]) {  // (of the norms)
   if (s[0] == 0 && s[1] == 0 && s[2] == 0)
     return Strided{{c.n[0], c.n[1], c.n[2]}, {(int64_t)c.n[1] * c.n[2] * c.C, (int64_t)c.n[2] * c.C, c.C}, c.C};
   return Strided{{c.n[0], c.n[1], c.n[2]}, {s[0], s[1], s[2]}, c.C};
@@ -359,11 +359,12 @@ constexpr int NORM_FWD_THREADS = 256, NORM_BWD_THREADS = 512;  // per workgroup,
 struct NormPlan {
   int ve, tpr, p;
 };
-// `align`: every row of every tensor starts at, and C is, a multiple of so many elements.
-inline NormPlan norm_plan(const mita_norm_cfg_t &c, int align) {
-  const int full = 16 / (int)elem_bytes(c);
+// `align`: every row of every tensor starts at, and C is, a multiple of so many
+// elements, of `bytes` each.
+inline NormPlan row_plan(size_t bytes, int C, int align) {
+  const int full = 16 / (int)bytes;
   const int ve = align % full == 0 ? full : align % 2 == 0 ? 2 : 1;
-  const int n = c.C / ve;  // pieces
+  const int n = C / ve;  // pieces
   if (ve == full) {
     // within a wave: the fewest idle lanes (768 bf16 elements: 32 threads of three
     // pieces), then the fewest registers
@@ -378,12 +379,14 @@ inline NormPlan norm_plan(const mita_norm_cfg_t &c, int align) {
   }
   return {ve, 256, 0};
 }
-// Workgroups of the backward, each with a partial sum of dw and db: two per CU,
-// or fewer where the rows do not fill them.
-inline int norm_bwd_blocks(const mita_norm_cfg_t &c, const NormPlan &p) {
+inline NormPlan norm_plan(const mita_norm_cfg_t &c, int align) { return row_plan(elem_bytes(c), c.C, align); }
+// Workgroups of the backward, each with a partial sum of the weights' gradients: two
+// per CU, or fewer where the rows do not fill them.
+inline int row_bwd_blocks(int64_t rows, const NormPlan &p) {
   const int64_t per = p.p ? std::max(1, NORM_BWD_THREADS / p.tpr) : 64;
-  return (int)std::min<int64_t>((norm_rows(c) + per - 1) / per, 2 * CUS);
+  return (int)std::min<int64_t>((rows + per - 1) / per, 2 * CUS);
 }
+inline int norm_bwd_blocks(const mita_norm_cfg_t &c, const NormPlan &p) { return row_bwd_blocks(norm_rows(c), p); }
 inline size_t norm_workspace_size(const mita_norm_cfg_t *c) {
   if (check_norm(c, nullptr) != MITA_OK) return 0;
   // how rows are aligned is known only with the pointers
@@ -391,6 +394,133 @@ inline size_t norm_workspace_size(const mita_norm_cfg_t *c) {
   for (int align = 1; align <= 8; align *= 2)
     if (c->C % align == 0) n = std::max(n, norm_bwd_blocks(*c, norm_plan(*c, align)));
   return align_up((size_t)n * 2 * c->C * sizeof(float));
+}
+
+// ---------------------------------------------------------------------------
+// RMS norm with the residual's addition
+// ---------------------------------------------------------------------------
+constexpr int RMS_GROUP = 128;  // columns that share a scale of an 8-bit output
+inline size_t elem_bytes(const mita_rms_cfg_t &c) { return c.dtype == MITA_F32 ? 4 : 2; }
+inline size_t y_bytes(const mita_rms_cfg_t &c) { return c.ytype == MITA_E4M3 ? 1 : elem_bytes(c); }
+inline int64_t norm_rows(const mita_rms_cfg_t &c) { return (int64_t)c.n[0] * c.n[1] * c.n[2]; }
+inline int rms_scales(const mita_rms_cfg_t &c) {  // per row
+  return c.ytype != MITA_E4M3 ? 0 : c.group ? (c.C + c.group - 1) / c.group : 1;
+}
+
+inline int check_rms(const mita_rms_cfg_t *c, std::string *err) {
+  auto fail = [&](int st, const std::string &msg) {
+    if (err) *err = msg;
+    return st;
+  };
+  if (!c) return fail(MITA_ERR_INVALID_ARG, "cfg is NULL");
+  if (c->n[0] < 1 || c->n[1] < 1 || c->n[2] < 1 || c->C < 1) return fail(MITA_ERR_INVALID_ARG, "n and C must be >= 1");
+  for (int t : {c->dtype, c->wdtype})
+    if (t != MITA_F32 && t != MITA_BF16)
+      return fail(MITA_ERR_UNSUPPORTED, "dtype and wdtype must be MITA_F32 or MITA_BF16");
+  if (c->ytype != c->dtype && c->ytype != MITA_E4M3)
+    return fail(MITA_ERR_UNSUPPORTED, "ytype must be dtype or MITA_E4M3");
+  if (c->group != 0 && (c->group != RMS_GROUP || c->ytype != MITA_E4M3))
+    return fail(MITA_ERR_UNSUPPORTED, "group must be 0, or 128 with MITA_E4M3");
+  if (c->C > MITA_NORM_MAX_C) return fail(MITA_ERR_UNSUPPORTED, "C must not exceed MITA_NORM_MAX_C");
+  if (!(c->eps > 0.f) || std::isinf(c->eps)) return fail(MITA_ERR_INVALID_ARG, "eps must be finite and > 0");
+  if ((int64_t)c->n[0] * c->n[1] > MITA_NORM_MAX_ROWS || norm_rows(*c) > MITA_NORM_MAX_ROWS)
+    return fail(MITA_ERR_UNSUPPORTED, "more than MITA_NORM_MAX_ROWS rows");
+  const struct {
+    const char *name;
+    const int64_t (&s)[3];
+    bool out;
+  } all[7] = {{"x", c->x, false},   {"res", c->res, false}, {"h", c->h, true},  {"y", c->y, true},
+              {"dy", c->dy, false}, {"dh", c->dh, false},   {"dx", c->dx, true}};
+  for (const auto &t : all) {
+    const Strided x = strided_rows(*c, t.s);
+    for (int i = 0; i < 3; ++i)
+      if (x.s[i] < 0 || x.s[i] > (int64_t)1 << 40)
+        return fail(MITA_ERR_INVALID_ARG, std::string("strides of ") + t.name + " must be in [0, 2^40]");
+    if (t.out && !nested(x))
+      return fail(MITA_ERR_INVALID_ARG, std::string("strides of ") + t.name + " give elements the same address");
+  }
+  return MITA_OK;
+}
+inline size_t rms_workspace_size(const mita_rms_cfg_t *c) {
+  if (check_rms(c, nullptr) != MITA_OK) return 0;
+  // how rows are aligned is known only with the pointers
+  int n = 0;
+  for (int align = 1; align <= 8; align *= 2)
+    if (c->C % align == 0) n = std::max(n, row_bwd_blocks(norm_rows(*c), row_plan(elem_bytes(*c), c->C, align)));
+  return align_up((size_t)n * c->C * sizeof(float));
+}
+
+// ---------------------------------------------------------------------------
+// Rotary positions
+// ---------------------------------------------------------------------------
+inline size_t elem_bytes(const mita_rope_cfg_t &c) { return c.dtype == MITA_F32 ? 4 : 2; }
+inline Strided strided_q(const mita_rope_cfg_t &c, const mita_strides_t &s0) {
+  const mita_strides_t s = strides_or(s0, c.H, c.N, c.d);
+  return Strided{{c.B, c.H, c.N}, {s.b, s.h, s.n}, c.d};
+}
+inline Strided strided_k(const mita_rope_cfg_t &c, const mita_strides_t &s0) {
+  const mita_strides_t s = strides_or(s0, c.H_kv, c.N, c.d);
+  return Strided{{c.B, c.H_kv, c.N}, {s.b, s.h, s.n}, c.d};
+}
+inline int check_rope(const mita_rope_cfg_t *c, std::string *err) {
+  auto fail = [&](int st, const std::string &msg) {
+    if (err) *err = msg;
+    return st;
+  };
+  if (!c) return fail(MITA_ERR_INVALID_ARG, "cfg is NULL");
+  if (c->B < 1 || c->H < 1 || c->H_kv < 1 || c->N < 1) return fail(MITA_ERR_INVALID_ARG, "B, H, H_kv, N must be >= 1");
+  if (c->dtype != MITA_F32 && c->dtype != MITA_BF16)
+    return fail(MITA_ERR_UNSUPPORTED, "dtype must be MITA_F32 or MITA_BF16");
+  if (c->d < 2) return fail(MITA_ERR_INVALID_ARG, "d must be >= 2");
+  if (c->d > MITA_ROPE_MAX_D) return fail(MITA_ERR_UNSUPPORTED, "d must not exceed MITA_ROPE_MAX_D");
+  if (c->rot < 2 || c->rot > c->d || c->rot % 2 != 0) return fail(MITA_ERR_INVALID_ARG, "rot must be even and in [2, d]");
+  if (c->H > 4096 || c->H_kv > 4096) return fail(MITA_ERR_UNSUPPORTED, "H and H_kv must not exceed 4096");
+  // a thread for each piece of a token, of which a launch has less than 2^32
+  if ((int64_t)c->B * c->N > (1 << 30) || (int64_t)c->B * c->N * c->d > ((int64_t)1 << 32) - 512)
+    return fail(MITA_ERR_UNSUPPORTED, "B * N * d must not exceed 2^32 - 512");
+  if (c->scaling < MITA_ROPE_NONE || c->scaling > MITA_ROPE_PARTS)
+    return fail(MITA_ERR_UNSUPPORTED, "scaling must be one of MITA_ROPE_*");
+  if (!(c->base > 1.0) || std::isinf(c->base)) return fail(MITA_ERR_INVALID_ARG, "base must be finite and > 1");
+  if (c->scaling != MITA_ROPE_NONE && (!(c->factor >= 1.0) || std::isinf(c->factor)))
+    return fail(MITA_ERR_INVALID_ARG, "factor must be finite and >= 1");
+  if (c->scaling == MITA_ROPE_BASE && c->rot < 4) return fail(MITA_ERR_INVALID_ARG, "MITA_ROPE_BASE needs rot >= 4");
+  if (c->scaling == MITA_ROPE_PARTS) {
+    if (c->trained < 1) return fail(MITA_ERR_INVALID_ARG, "trained must be >= 1");
+    if (!(c->slow >= 0.0) || !(c->fast > c->slow) || std::isinf(c->fast))
+      return fail(MITA_ERR_INVALID_ARG, "slow and fast must be finite with 0 <= slow < fast");
+  }
+  if (!(c->scale >= 0.f) || std::isinf(c->scale)) return fail(MITA_ERR_INVALID_ARG, "scale must be finite and >= 0");
+  if (c->pos_b != 0 && c->pos_b != c->N) return fail(MITA_ERR_INVALID_ARG, "pos_b must be 0 or N");
+  if (c->first < -((int64_t)1 << 31) || c->first > (int64_t)1 << 31)
+    return fail(MITA_ERR_INVALID_ARG, "first must be in [-2^31, 2^31]");
+  const struct {
+    const char *name;
+    const mita_strides_t *s;
+    bool key, out;
+  } all[4] = {{"q", &c->q, false, false}, {"k", &c->k, true, false}, {"qo", &c->qo, false, true}, {"ko", &c->ko, true, true}};
+  for (const auto &t : all) {
+    const Strided x = t.key ? strided_k(*c, *t.s) : strided_q(*c, *t.s);
+    for (int i = 0; i < 3; ++i)
+      if (x.s[i] < 0 || x.s[i] > (int64_t)1 << 40)
+        return fail(MITA_ERR_INVALID_ARG, std::string("strides of ") + t.name + " must be in [0, 2^40]");
+    if (t.out && !nested(x))
+      return fail(MITA_ERR_INVALID_ARG, std::string("strides of ") + t.name + " give elements the same address");
+  }
+  return MITA_OK;
+}
+// Turns per position of each pair, rot / 2 of them.
+inline void rope_turns(const mita_rope_cfg_t &c, double *f) {
+  const double two_pi = 6.283185307179586476925286766559, base =
+      c.scaling == MITA_ROPE_BASE ? c.base * std::pow(c.factor, (double)c.rot / (c.rot - 2)) : c.base;
+  for (int i = 0; i < c.rot / 2; ++i) {
+    double t = std::pow(base, -2.0 * i / c.rot) / two_pi;
+    if (c.scaling == MITA_ROPE_LINEAR) t /= c.factor;
+    if (c.scaling == MITA_ROPE_PARTS) {
+      const double keep = std::min(1.0, std::max(0.0, (c.trained * t - c.slow) / (c.fast - c.slow)));
+      t = keep * t + (1.0 - keep) * t / c.factor;
+    }
+    f[i] = t;
+  }
 }
 
 }  // namespace mita

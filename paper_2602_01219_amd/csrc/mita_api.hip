@@ -378,6 +378,17 @@ int validate(const mita_norm_cfg_t *c) {
   return st == MITA_OK ? st : set_err(st, msg);
 }
 
+int validate(const mita_rms_cfg_t *c) {
+  std::string msg;
+  const int st = check_rms(c, &msg);
+  return st == MITA_OK ? st : set_err(st, msg);
+}
+int validate(const mita_rope_cfg_t *c) {
+  std::string msg;
+  const int st = check_rope(c, &msg);
+  return st == MITA_OK ? st : set_err(st, msg);
+}
+
 int need_bytes(size_t need, const void *ws, size_t ws_bytes) {
   if (need == 0) return MITA_OK;
   if (!ws || ws_bytes < need)
@@ -415,6 +426,31 @@ int apart(std::initializer_list<Buffer> out, std::initializer_list<Buffer> in) {
       if (overlap(*a, *b)) return set_err(MITA_ERR_INVALID_ARG, std::string(a->name) + " overlaps " + b->name);
   }
   return MITA_OK;
+}
+
+int rope(const mita_rope_cfg_t *cfg, const void *q, const void *k, const int32_t *pos, void *qo, void *ko, bool back,
+         hipStream_t st) {
+  TRY(validate(cfg));
+  const size_t e = elem_bytes(*cfg);
+  TRY(need_elem_ptr(q, e, back ? "dqo" : "q"));
+  TRY(need_elem_ptr(qo, e, back ? "dq" : "qo"));
+  if (!k != !ko) return set_err(MITA_ERR_INVALID_ARG, "one of the keys' tensors is NULL and the other is not");
+  if (k) {
+    TRY(need_elem_ptr(k, e, back ? "dko" : "k"));
+    TRY(need_elem_ptr(ko, e, back ? "dk" : "ko"));
+  }
+  if (pos) TRY(need_elem_ptr(pos, 4, "pos"));
+  const Strided sq = strided_q(*cfg, cfg->q), sk = strided_k(*cfg, cfg->k);
+  const Strided sqo = strided_q(*cfg, cfg->qo), sko = strided_k(*cfg, cfg->ko);
+  const Buffer bq{"the queries", q, sq, e}, bk{"the keys", k, sk, e};
+  const Buffer bqo{"the queries' output", qo, sqo, e}, bko{"the keys' output", ko, sko, e};
+  const Buffer bp = bytes_of("pos", pos, (size_t)(cfg->pos_b ? cfg->B : 1) * cfg->N * 4);
+  if (!same_rows(q, sq, qo, sqo)) TRY(apart({bqo}, {bq}));
+  if (k && !same_rows(k, sk, ko, sko)) TRY(apart({bko}, {bk}));
+  TRY(apart({bqo, bko}, {bp}));
+  TRY(apart({bqo}, {bk}));
+  TRY(apart({bko}, {bq}));
+  return hip_status(launch_rope(*cfg, q, k, pos, qo, ko, back, st), back ? "rope backward" : "rope forward");
 }
 
 // Nothing is thrown across the ABI (building a message may run out of memory).
@@ -803,6 +839,86 @@ int mita_norm_backward(const mita_norm_cfg_t *cfg, const void *x, const void *w,
     return hip_status(launch_norm_backward(*cfg, x, w, mean, rstd, dy, dx, dw, db, ws, (hipStream_t)stream),
                       "norm backward");
   });
+}
+
+int mita_rms_check(const mita_rms_cfg_t *cfg) {
+  return guarded([&]() -> int { return validate(cfg); });
+}
+
+size_t mita_rms_workspace_size(const mita_rms_cfg_t *cfg) {
+  return guarded_size([&]() -> size_t { return rms_workspace_size(cfg); });
+}
+
+int mita_rms_forward(const mita_rms_cfg_t *cfg, const void *x, const void *res, const void *w, void *h, void *y,
+                     float *scales, float *rstd, mita_stream_t stream) {
+  return guarded([&]() -> int {
+    TRY(validate(cfg));
+    const size_t e = elem_bytes(*cfg), ey = y_bytes(*cfg), ew = cfg->wdtype == MITA_F32 ? 4 : 2;
+    const size_t rows = (size_t)norm_rows(*cfg);
+    TRY(need_elem_ptr(x, e, "x"));
+    TRY(need_elem_ptr(y, ey, "y"));
+    if (res) TRY(need_elem_ptr(res, e, "res"));
+    if (w) TRY(need_elem_ptr(w, ew, "w"));
+    if (h) TRY(need_elem_ptr(h, e, "h"));
+    if (cfg->ytype == MITA_E4M3) TRY(need_elem_ptr(scales, 4, "scales"));
+    if (cfg->ytype != MITA_E4M3 && scales) return set_err(MITA_ERR_INVALID_ARG, "scales are given, but y is not in 8 bits");
+    if (rstd) TRY(need_elem_ptr(rstd, 4, "rstd"));
+    const Strided sx = strided_rows(*cfg, cfg->x), sr = strided_rows(*cfg, cfg->res);
+    const Strided sh = strided_rows(*cfg, cfg->h), sy = strided_rows(*cfg, cfg->y);
+    const Buffer bx{"x", x, sx, e}, bres{"res", res, sr, e}, bh{"h", h, sh, e}, by{"y", y, sy, ey};
+    const Buffer bw = bytes_of("w", w, cfg->C * ew), bs = bytes_of("scales", scales, rows * rms_scales(*cfg) * 4);
+    const Buffer br = bytes_of("rstd", rstd, rows * 4);
+    const bool wide = ey == e;  // y's elements are as wide as the inputs': it may take their place
+    if (!same_rows(x, sx, h, sh)) TRY(apart({bh}, {bx}));
+    if (!same_rows(res, sr, h, sh)) TRY(apart({bh}, {bres}));
+    if (!wide || !same_rows(x, sx, y, sy)) TRY(apart({by}, {bx}));
+    if (!wide || !same_rows(res, sr, y, sy)) TRY(apart({by}, {bres}));
+    TRY(apart({by, bh, bs, br}, {bw}));
+    TRY(apart({bs, br}, {bx, bres}));
+    return hip_status(launch_rms_forward(*cfg, x, res, w, h, y, scales, rstd, (hipStream_t)stream), "rms forward");
+  });
+}
+
+int mita_rms_backward(const mita_rms_cfg_t *cfg, const void *h, const void *w, const float *rstd, const void *dy,
+                      const void *dh, void *dx, void *dw, void *ws, size_t ws_bytes, mita_stream_t stream) {
+  return guarded([&]() -> int {
+    TRY(validate(cfg));
+    const size_t e = elem_bytes(*cfg), ew = cfg->wdtype == MITA_F32 ? 4 : 2, rows = (size_t)norm_rows(*cfg);
+    TRY(need_elem_ptr(h, e, "h"));
+    TRY(need_elem_ptr(dy, e, "dy"));
+    TRY(need_elem_ptr(rstd, 4, "rstd"));
+    if (w) TRY(need_elem_ptr(w, ew, "w"));
+    if (dh) TRY(need_elem_ptr(dh, e, "dh"));
+    if (dx) TRY(need_elem_ptr(dx, e, "dx"));
+    if (dw) TRY(need_elem_ptr(dw, ew, "dw"));
+    if (!dx && !dw) return set_err(MITA_ERR_INVALID_ARG, "dx and dw are both NULL");
+    const size_t need = dw ? rms_workspace_size(cfg) : 0;
+    TRY(need_bytes(need, ws, ws_bytes));
+    const Strided sh = strided_rows(*cfg, cfg->h), sdy = strided_rows(*cfg, cfg->dy);
+    const Strided sdh = strided_rows(*cfg, cfg->dh), sdx = strided_rows(*cfg, cfg->dx);
+    const Buffer bh{"h", h, sh, e}, bdy{"dy", dy, sdy, e}, bdh{"dh", dh, sdh, e}, bdx{"dx", dx, sdx, e};
+    const Buffer bw = bytes_of("w", w, cfg->C * ew), br = bytes_of("rstd", rstd, rows * 4);
+    const Buffer bdw = bytes_of("dw", dw, cfg->C * ew), bws = bytes_of("ws", need ? ws : nullptr, need);
+    if (!same_rows(dy, sdy, dx, sdx)) TRY(apart({bdx}, {bdy}));
+    if (!same_rows(dh, sdh, dx, sdx)) TRY(apart({bdx}, {bdh}));
+    TRY(apart({bdx, bdw, bws}, {bh, bw, br}));
+    TRY(apart({bdw, bws}, {bdy, bdh}));
+    return hip_status(launch_rms_backward(*cfg, h, w, rstd, dy, dh, dx, dw, ws, (hipStream_t)stream), "rms backward");
+  });
+}
+
+int mita_rope_check(const mita_rope_cfg_t *cfg) {
+  return guarded([&]() -> int { return validate(cfg); });
+}
+
+int mita_rope_forward(const mita_rope_cfg_t *cfg, const void *q, const void *k, const int32_t *pos, void *qo, void *ko,
+                      mita_stream_t stream) {
+  return guarded([&]() -> int { return rope(cfg, q, k, pos, qo, ko, false, (hipStream_t)stream); });
+}
+
+int mita_rope_backward(const mita_rope_cfg_t *cfg, const void *dqo, const void *dko, const int32_t *pos, void *dq,
+                       void *dk, mita_stream_t stream) {
+  return guarded([&]() -> int { return rope(cfg, dqo, dko, pos, dq, dk, true, (hipStream_t)stream); });
 }
 
 int mita_timer_create(mita_timer_t **timer, int max_calls) {

@@ -313,32 +313,6 @@ template <typename T, int VE, int TPR, int P> hipError_t bwd_p(const NormArgs &a
   return launched("norm_bwd_kernel", st);
 }
 
-// f.run<VE, TPR, P>() for the plan's geometry
-template <int VE, typename F> hipError_t with_plan_odd(const NormPlan &p, F &f) {
-  if (p.tpr == 64) {
-    if (p.p <= 4) return p.p == 2 ? f.template run<VE, 64, 2>() : f.template run<VE, 64, 4>();
-    return p.p == 6 ? f.template run<VE, 64, 6>() : f.template run<VE, 64, 8>();
-  }
-  if (p.tpr == 256) return p.p == 4 ? f.template run<VE, 256, 4>() : f.template run<VE, 256, 8>();
-  return f.template run<VE, 1024, 8>();
-}
-template <typename T, typename F> hipError_t with_plan(const NormPlan &p, F &&f) {
-  constexpr int V = 16 / (int)sizeof(T);
-  if (p.ve == V) {
-    if (p.tpr == 8) return f.template run<V, 8, 1>();
-    if (p.tpr == 16) return p.p == 1 ? f.template run<V, 16, 1>() : f.template run<V, 16, 3>();
-    if (p.tpr == 32) return p.p == 1 ? f.template run<V, 32, 1>() : f.template run<V, 32, 3>();
-    if (p.tpr == 64) {
-      if (p.p == 1) return f.template run<V, 64, 1>();
-      if (p.p == 2) return f.template run<V, 64, 2>();
-      if (p.p == 3) return f.template run<V, 64, 3>();
-      return f.template run<V, 64, 4>();
-    }
-    if (p.tpr == 256) return p.p == 2 ? f.template run<V, 256, 2>() : f.template run<V, 256, 4>();
-    return f.template run<V, 1024, 2>();
-  }
-  return p.ve == 2 ? with_plan_odd<2>(p, f) : with_plan_odd<1>(p, f);
-}
 template <typename T> struct RunFwd {
   const NormArgs &a;
   hipStream_t st;

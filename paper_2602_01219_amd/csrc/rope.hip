@@ -1,0 +1,228 @@
+// rope.hip - rotary positions of queries and keys: (u, v) -> s (u cos a - v sin a,
+// v cos a + u sin a) with a = pos f_i for each pair of a head's first elements, and its
+// transpose for the gradients.
+//
+// Bound by HBM: every element is read and written once. A thread turns the same
+// piece (of 16 bytes, or two of them where a head's halves form the pairs) of
+// several heads of one token, so its angles' sines and cosines are formed once for
+// all of them.
+#include "cdna4.hpp"
+#include "kernels.hpp"
+#include "layer_check.hpp"
+
+namespace mita {
+
+namespace {
+
+struct RopeMat {
+  const char *in;
+  char *out;
+  int64_t ib, ih, in_n, ob, oh, on;  // bytes between batch elements, heads and tokens
+  int heads;
+  bool same;  // out is in: elements that do not turn stay where they are
+};
+struct RopeArgs {
+  RopeMat m[2];  // queries, keys
+  const int32_t *pos;
+  int pos_b;
+  int B, N, items;   // items: pieces of a token that a thread takes
+  int turning;       // of these, the first so many turn
+  int rot, heads, per;  // heads in all, and of a thread
+  int64_t first;
+  float scale;
+  double f[MITA_ROPE_MAX_D / 2];  // turns per position
+};
+
+// Sine and cosine of `turns` whole turns: reduced to an eighth of a turn around a
+// quarter in 64 bits (exactly, for turns below 2^53), then Taylor sums, whose next
+// terms are below 2^-27 of the largest value.
+__device__ __forceinline__ void sin_cos_turns(double turns, float &s, float &c) {
+  const double r = turns - rint(turns), q = rint(4.0 * r);
+  const float x = (float)(r - 0.25 * q) * 6.2831853071795865f, y = x * x;
+  float sn = __builtin_fmaf(y, 2.7557319e-6f, -1.9841270e-4f);
+  sn = __builtin_fmaf(y, sn, 8.3333333e-3f);
+  sn = __builtin_fmaf(y, sn, -1.6666667e-1f);
+  sn = __builtin_fmaf(x * y, sn, x);
+  float cs = __builtin_fmaf(y, -2.7557319e-7f, 2.4801587e-5f);
+  cs = __builtin_fmaf(y, cs, -1.3888889e-3f);
+  cs = __builtin_fmaf(y, cs, 4.1666667e-2f);
+  cs = __builtin_fmaf(y, cs, -0.5f);
+  cs = __builtin_fmaf(y, cs, 1.f);
+  const int k = (int)q;
+  const float a = k & 1 ? cs : sn, b = k & 1 ? sn : cs;
+  s = k & 2 ? -a : a;
+  c = (k + 1) & 2 ? -b : b;
+}
+
+template <typename T, int V> __device__ __forceinline__ void get(const char *p, float (&f)[V]) {
+  constexpr int BYTES = V * (int)sizeof(T);
+  if constexpr (BYTES == 16) {
+    unpack16(*reinterpret_cast<const uint4 *>(p), f, (const T *)nullptr);
+  } else if constexpr (BYTES == 8 && sizeof(T) == 4) {
+    const float2 x = *reinterpret_cast<const float2 *>(p);
+    f[0] = x.x;
+    f[1] = x.y;
+  } else if constexpr (BYTES == 4 && sizeof(T) == 2) {
+    const uint32_t x = *reinterpret_cast<const uint32_t *>(p);
+    f[0] = __uint_as_float(x << 16);
+    f[1] = __uint_as_float(x & 0xffff0000u);
+  } else {
+    static_assert(V == 1, "16 bytes, two elements or one");
+    f[0] = to_f32(*reinterpret_cast<const T *>(p));
+  }
+}
+template <typename T, int V> __device__ __forceinline__ void put(char *p, const float (&f)[V]) {
+  constexpr int BYTES = V * (int)sizeof(T);
+  if constexpr (BYTES == 16 && sizeof(T) == 4) {
+    *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  } else if constexpr (BYTES == 16) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
+                                               pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+  } else if constexpr (BYTES == 8 && sizeof(T) == 4) {
+    *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
+  } else if constexpr (BYTES == 4 && sizeof(T) == 2) {
+    *reinterpret_cast<uint32_t *>(p) = pack_bf16x2(f[0], f[1]);
+  } else {
+    *reinterpret_cast<T *>(p) = from_f32<T>(f[0]);
+  }
+}
+
+__device__ __forceinline__ void turn(float &u, float &v, float sn, float cs) {
+  const float y = u, z = v;
+  u = __builtin_fmaf(y, cs, -(z * sn));
+  v = __builtin_fmaf(z, cs, y * sn);
+}
+
+// Thread x of the grid takes piece x % items of token x / items, of the heads that
+// blockIdx.y gives it. Items below `turning` turn: V pairs of two pieces V long and
+// rot / 2 apart, or (IL) the V / 2 pairs of one piece (V = 1: of two elements). The
+// others are V elements that are copied.
+template <typename T, int V, bool IL> __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
+  constexpr int NP = IL ? (V > 1 ? V / 2 : 1) : V;  // pairs of an item
+  const uint32_t x = blockIdx.x * 256 + threadIdx.x, t = x / (uint32_t)a.items;
+  const int token = (int)t, item = (int)(x - t * (uint32_t)a.items);
+  if (token >= a.B * a.N) return;
+  const int b = token / a.N, n = token - b * a.N;
+  const bool turns = item < a.turning;
+  // the first element of the item, and where its pairs' other elements are
+  const int e0 = turns ? (IL ? 2 * NP * item : V * item) : a.rot + V * (item - a.turning);
+  const int apart = turns && !IL ? (a.rot / 2) * (int)sizeof(T) : 0;
+  float sn[NP], cs[NP];
+  if (turns) {
+    const double p = a.pos ? (double)a.pos[(int64_t)b * a.pos_b + n] : (double)(a.first + n);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      sin_cos_turns(p * a.f[item * NP + i], sn[i], cs[i]);
+      sn[i] *= a.scale;
+      cs[i] *= fabsf(a.scale);
+    }
+  }
+  const int h0 = blockIdx.y * a.per, h1 = min(a.heads, h0 + a.per);
+  for (int hh = h0; hh < h1; ++hh) {
+    const bool key = hh >= a.m[0].heads;
+    const RopeMat &m = a.m[key];
+    const int h = key ? hh - a.m[0].heads : hh;
+    const char *src = m.in + b * m.ib + h * m.ih + n * m.in_n + e0 * (int)sizeof(T);
+    char *dst = m.out + b * m.ob + h * m.oh + n * m.on + e0 * (int)sizeof(T);
+    if (!turns) {
+      if (m.same) continue;
+      float u[V];
+      get<T, V>(src, u);
+      put<T, V>(dst, u);
+      continue;
+    }
+    if constexpr (IL && V == 1) {
+      float u[1], v[1];
+      get<T, 1>(src, u);
+      get<T, 1>(src + sizeof(T), v);
+      turn(u[0], v[0], sn[0], cs[0]);
+      put<T, 1>(dst, u);
+      put<T, 1>(dst + sizeof(T), v);
+    } else if constexpr (IL) {
+      float u[V];
+      get<T, V>(src, u);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) turn(u[2 * i], u[2 * i + 1], sn[i], cs[i]);
+      put<T, V>(dst, u);
+    } else {
+      float u[V], v[V];
+      get<T, V>(src, u);
+      get<T, V>(src + apart, v);
+#pragma unroll
+      for (int i = 0; i < V; ++i) turn(u[i], v[i], sn[i], cs[i]);
+      put<T, V>(dst, u);
+      put<T, V>(dst + apart, v);
+    }
+  }
+}
+
+// The largest of 16 bytes, two elements and one that every piece of both tensors is
+// aligned to.
+int rope_vector(const mita_rope_cfg_t &c, const Strided *t, const void *const *p) {
+  const int e = (int)elem_bytes(c), full = 16 / e;
+  auto fits = [&](int v) {
+    if (c.d % v != 0 || c.rot % v != 0 || (!c.interleaved && (c.rot / 2) % v != 0)) return false;
+    for (int i = 0; i < 4; ++i) {
+      if (!p[i]) continue;
+      if ((uintptr_t)p[i] % (v * e) != 0) return false;
+      for (int k = 0; k < 3; ++k)
+        if (t[i].n[k] > 1 && t[i].s[k] % v != 0) return false;
+    }
+    return true;
+  };
+  return fits(full) ? full : fits(2) ? 2 : 1;
+}
+
+template <typename T, int V> hipError_t rope_v(const RopeArgs &a, bool il, dim3 grid, hipStream_t st) {
+  if (il)
+    rope_kernel<T, V, true><<<grid, 256, 0, st>>>(a);
+  else
+    rope_kernel<T, V, false><<<grid, 256, 0, st>>>(a);
+  return launched("rope_kernel", st);
+}
+
+}  // namespace
+
+hipError_t launch_rope(const mita_rope_cfg_t &c, const void *q, const void *k, const int32_t *pos, void *qo, void *ko,
+                       bool back, hipStream_t st) {
+  const Strided t[4] = {strided_q(c, c.q), strided_k(c, c.k), strided_q(c, c.qo), strided_k(c, c.ko)};
+  const void *const p[4] = {q, k, qo, ko};
+  const int e = (int)elem_bytes(c), v = rope_vector(c, t, p);
+  RopeArgs a{};
+  for (int i = 0; i < 2; ++i) {
+    const Strided &x = t[i], &y = t[2 + i];
+    a.m[i] = RopeMat{(const char *)p[i],
+                     (char *)const_cast<void *>(p[2 + i]),
+                     x.s[0] * e,
+                     x.s[1] * e,
+                     x.s[2] * e,
+                     y.s[0] * e,
+                     y.s[1] * e,
+                     y.s[2] * e,
+                     i == 0 ? c.H : k ? c.H_kv : 0,
+                     p[i] == p[2 + i]};
+  }
+  a.pos = pos;
+  a.pos_b = c.pos_b;
+  a.B = c.B;
+  a.N = c.N;
+  a.rot = c.rot;
+  const int pairs = c.interleaved ? std::max(1, v / 2) : v;
+  a.turning = c.rot / 2 / pairs;
+  a.items = a.turning + (a.m[0].same && (!k || a.m[1].same) ? 0 : (c.d - c.rot) / v);
+  a.first = c.first;
+  const float scale = c.scale != 0.f ? c.scale : 1.f;
+  a.scale = back ? -scale : scale;
+  a.heads = c.H + a.m[1].heads;
+  rope_turns(c, a.f);
+  const int64_t threads = (int64_t)c.B * c.N * a.items;
+  // as many heads per thread as leave eight waves per SIMD
+  a.per = (int)std::max<int64_t>(1, std::min<int64_t>(a.heads, threads * a.heads / (8 * 4 * 64 * CUS)));
+  const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)((a.heads + a.per - 1) / a.per));
+  const bool il = c.interleaved != 0;
+  if (c.dtype == MITA_F32)
+    return v == 4 ? rope_v<float, 4>(a, il, grid, st) : v == 2 ? rope_v<float, 2>(a, il, grid, st) : rope_v<float, 1>(a, il, grid, st);
+  return v == 8 ? rope_v<bf16_t, 8>(a, il, grid, st) : v == 2 ? rope_v<bf16_t, 2>(a, il, grid, st) : rope_v<bf16_t, 1>(a, il, grid, st);
+}
+
+}  // namespace mita

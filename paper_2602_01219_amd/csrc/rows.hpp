@@ -141,6 +141,27 @@ template <int W> __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
+// The largest of x over the lanes of a group of W, the same in each (NaN is passed over).
+template <int W> __device__ __forceinline__ float group_max(float x) {
+  auto dpp = [](float v, auto ctrl) {
+    return __uint_as_float(
+        (uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x = fmaxf(x, dpp(x, std::integral_constant<int, 0xb1>{}));
+  x = fmaxf(x, dpp(x, std::integral_constant<int, 0x4e>{}));
+  x = fmaxf(x, dpp(x, std::integral_constant<int, 0x141>{}));
+  if constexpr (W >= 16) x = fmaxf(x, dpp(x, std::integral_constant<int, 0x140>{}));
+  if constexpr (W >= 32) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  }
+  if constexpr (W >= 64) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  }
+  return x;
+}
+
 // Sums over the TPR threads of a row. Those of several waves go through `red`,
 // whose halves consecutive calls use in turn.
 template <int TPR, int THREADS, int K> struct RowSum {
@@ -230,4 +251,30 @@ inline RowWalk row_walk(const Strided *t, int tensors, RowPlaces *places) {
   return a;
 }
 
+// f.run<VE, TPR, P>() for the plan's geometry
+template <int VE, typename F> hipError_t with_plan_odd(const NormPlan &p, F &f) {
+  if (p.tpr == 64) {
+    if (p.p <= 4) return p.p == 2 ? f.template run<VE, 64, 2>() : f.template run<VE, 64, 4>();
+    return p.p == 6 ? f.template run<VE, 64, 6>() : f.template run<VE, 64, 8>();
+  }
+  if (p.tpr == 256) return p.p == 4 ? f.template run<VE, 256, 4>() : f.template run<VE, 256, 8>();
+  return f.template run<VE, 1024, 8>();
+}
+template <typename T, typename F> hipError_t with_plan(const NormPlan &p, F &&f) {
+  constexpr int V = 16 / (int)sizeof(T);
+  if (p.ve == V) {
+    if (p.tpr == 8) return f.template run<V, 8, 1>();
+    if (p.tpr == 16) return p.p == 1 ? f.template run<V, 16, 1>() : f.template run<V, 16, 3>();
+    if (p.tpr == 32) return p.p == 1 ? f.template run<V, 32, 1>() : f.template run<V, 32, 3>();
+    if (p.tpr == 64) {
+      if (p.p == 1) return f.template run<V, 64, 1>();
+      if (p.p == 2) return f.template run<V, 64, 2>();
+      if (p.p == 3) return f.template run<V, 64, 3>();
+      return f.template run<V, 64, 4>();
+    }
+    if (p.tpr == 256) return p.p == 2 ? f.template run<V, 256, 2>() : f.template run<V, 256, 4>();
+    return f.template run<V, 1024, 2>();
+  }
+  return p.ve == 2 ? with_plan_odd<2>(p, f) : with_plan_odd<1>(p, f);
+}
 }  // namespace mita

@@ -24,7 +24,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libmita.so")
 
 MITA_OK, MITA_ERR_INVALID_ARG, MITA_ERR_UNSUPPORTED, MITA_ERR_WORKSPACE, MITA_ERR_HIP = range(5)
-MITA_F32, MITA_BF16 = 0, 1
+MITA_F32, MITA_BF16, MITA_E4M3 = 0, 1, 2
+ROPE_SCALINGS = ("none", "linear", "base", "parts")
 MITA_FLAG_STAGED_GATHER = 0x1
 MITA_FLAG_FULL_SCORES = 0x2
 WS_FORWARD, WS_SCORES, WS_TOPK, WS_ROUTE, WS_ATTEND, WS_BACKWARD, WS_TOME = range(7)
@@ -41,7 +42,9 @@ EXPORTED = ("mita_check", "mita_workspace_size", "mita_status_string", "mita_las
             "mita_forward_noalloc", "mita_landmarks_select", "mita_forward_lm", "mita_forward_lm_timed",
             "mita_backward", "mita_backward_timed", "mita_landmarks_tome",
             "mita_dense_check", "mita_dense_workspace_size", "mita_dense_forward", "mita_dense_backward",
-            "mita_norm_check", "mita_norm_workspace_size", "mita_norm_forward", "mita_norm_backward")
+            "mita_norm_check", "mita_norm_workspace_size", "mita_norm_forward", "mita_norm_backward",
+            "mita_rms_check", "mita_rms_workspace_size", "mita_rms_forward", "mita_rms_backward",
+            "mita_rope_check", "mita_rope_forward", "mita_rope_backward")
 
 
 class CfgStruct(ctypes.Structure):
@@ -67,6 +70,20 @@ class NormCfgStruct(ctypes.Structure):
                 ("dx", ctypes.c_int64 * 3)]
 
 
+class RmsCfgStruct(ctypes.Structure):
+    _fields_ = ([("n", ctypes.c_int32 * 3)] + [(n, ctypes.c_int32) for n in ("C", "dtype", "wdtype", "ytype", "group")]
+                + [("eps", ctypes.c_float)]
+                + [(n, ctypes.c_int64 * 3) for n in ("x", "res", "h", "y", "dy", "dh", "dx")])
+
+
+class RopeCfgStruct(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in
+                 ("B", "H", "H_kv", "N", "d", "rot", "dtype", "interleaved", "scaling", "trained")]
+                + [(n, ctypes.c_double) for n in ("base", "factor", "slow", "fast")]
+                + [("scale", ctypes.c_float), ("pos_b", ctypes.c_int32), ("first", ctypes.c_int64)]
+                + [(n, StridesStruct) for n in ("q", "k", "qo", "ko")])
+
+
 class MitaError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"mita status {status}: {msg}")
@@ -87,6 +104,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     P, I, Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
     cfgp = ctypes.POINTER(CfgStruct)
     densep, normp = ctypes.POINTER(DenseCfgStruct), ctypes.POINTER(NormCfgStruct)
+    rmsp, ropep = ctypes.POINTER(RmsCfgStruct), ctypes.POINTER(RopeCfgStruct)
     sig = {
         "mita_check": (I, [cfgp]),
         "mita_workspace_size": (Z, [cfgp, I]),
@@ -113,6 +131,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "mita_norm_workspace_size": (Z, [normp]),
         "mita_norm_forward": (I, [normp, P, P, P, P, P, P, P]),
         "mita_norm_backward": (I, [normp, P, P, P, P, P, P, P, P, P, Z, P]),
+        "mita_rms_check": (I, [rmsp]),
+        "mita_rms_workspace_size": (Z, [rmsp]),
+        "mita_rms_forward": (I, [rmsp, P, P, P, P, P, P, P, P]),
+        "mita_rms_backward": (I, [rmsp, P, P, P, P, P, P, P, P, Z, P]),
+        "mita_rope_check": (I, [ropep]),
+        "mita_rope_forward": (I, [ropep, P, P, P, P, P, P]),
+        "mita_rope_backward": (I, [ropep, P, P, P, P, P, P]),
         "mita_topk": (I, [cfgp, P, P, P, Z, P]),
         "mita_gather": (I, [cfgp, P, P, P, P, P, P]),
         "mita_route": (I, [cfgp, P, P, P, P, P, P, Z, P]),
@@ -456,19 +481,115 @@ class NormConfig(_Planned):
         return torch.float32 if self.wdtype == "f32" else torch.bfloat16
 
     def struct(self, **tensors) -> NormCfgStruct:
-        if not 1 <= len(self.rows) <= 3:
-            raise ValueError("rows must have one to three dimensions")
-        pad = 3 - len(self.rows)
-        c = NormCfgStruct()
-        c.n = (ctypes.c_int32 * 3)(*([1] * pad + [_int32("rows", n) for n in self.rows]))
-        c.C, c.eps = _int32("C", self.C), _fp32("eps", self.eps)
-        c.dtype, c.wdtype = _dtype_code(self.dtype), _dtype_code(self.wdtype)
-        for name, t in tensors.items():
-            s = [0] * pad + _row_strides(t)
-            if any(s):
-                # dimensions in front of the rows have one entry: any distance will do
-                setattr(c, name, (ctypes.c_int64 * 3)(*[x or self.C for x in s[:pad]], *s[pad:]))
+        return _rows_struct(NormCfgStruct(), self, tensors)
+
+
+@dataclass(frozen=True)
+class RmsConfig(_Planned):
+    """RMS norm of rows of C elements with the residual's addition
+    (mita_rms_cfg_t without the strides): rows is the shape in front of the last
+    dimension, up to three dimensions. out = "e4m3" gives y in 8 bits, with a scale
+    for each `group` (128) columns, or with group = 0 for each row."""
+    rows: tuple
+    C: int
+    dtype: str = "bf16"          # x, res, h and their gradients; y's with out = "same"
+    wdtype: str = "f32"          # weight and its gradient
+    out: str = "same"            # "same" | "e4m3"
+    group: int = 0
+    eps: float = 1e-5
+
+    @property
+    def shape(self):
+        return tuple(self.rows) + (self.C,)
+
+    @property
+    def scales_shape(self):
+        return tuple(self.rows) + (-(-self.C // self.group) if self.group else 1,)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == "f32" else torch.bfloat16
+
+    @property
+    def torch_wdtype(self):
+        return torch.float32 if self.wdtype == "f32" else torch.bfloat16
+
+    @property
+    def torch_ydtype(self):
+        return torch.float8_e4m3fn if self.out == "e4m3" else self.torch_dtype
+
+    def struct(self, **tensors) -> RmsCfgStruct:
+        if self.out not in ("same", "e4m3"):
+            raise ValueError(f"out must be 'same' or 'e4m3', got {self.out!r}")
+        c = _rows_struct(RmsCfgStruct(), self, tensors)
+        c.ytype = MITA_E4M3 if self.out == "e4m3" else c.dtype
+        c.group = _int32("group", self.group)
         return c
+
+
+@dataclass(frozen=True)
+class RopeConfig(_Planned):
+    """Rotary positions of queries [B, H, N, d] and keys [B, H_kv, N, d]
+    (mita_rope_cfg_t without the strides). H_kv = 0 means H, rot = 0 means d."""
+    B: int
+    H: int
+    N: int
+    d: int
+    H_kv: int = 0
+    rot: int = 0
+    dtype: str = "bf16"          # "f32" | "bf16"
+    interleaved: bool = False    # pairs of neighbours, else of the two halves of the rotated part
+    base: float = 10000.0
+    scaling: str = "none"        # "none" | "linear" | "base" | "parts"
+    factor: float = 1.0
+    trained: int = 0             # "parts": positions of training,
+    slow: float = 1.0            # turns over these up to which a pair is stretched whole,
+    fast: float = 32.0           # and from which on it is not
+    scale: float = 0.0           # of the rotated elements; 0 -> 1
+    first: int = 0               # position of token 0 where no positions are given
+
+    @property
+    def q_shape(self):
+        return (self.B, self.H, self.N, self.d)
+
+    @property
+    def k_shape(self):
+        return (self.B, self.H_kv or self.H, self.N, self.d)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == "f32" else torch.bfloat16
+
+    def struct(self, pos_b: int = 0, **tensors) -> RopeCfgStruct:
+        if self.scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling must be one of {ROPE_SCALINGS}, got {self.scaling!r}")
+        B, H, N, d = (_int32(n, getattr(self, n)) for n in ("B", "H", "N", "d"))
+        first = operator.index(self.first)
+        if abs(first) > 2 ** 31:
+            raise ValueError(f"first = {first} is beyond 2^31")
+        c = RopeCfgStruct(B, H, _int32("H_kv", self.H_kv) or H, N, d, _int32("rot", self.rot) or d,
+                          _dtype_code(self.dtype), int(bool(self.interleaved)), ROPE_SCALINGS.index(self.scaling),
+                          _int32("trained", self.trained), float(self.base), float(self.factor), float(self.slow),
+                          float(self.fast), _fp32("scale", self.scale), pos_b, first)
+        for name, t in tensors.items():
+            setattr(c, name, StridesStruct(*_row_strides(t)))
+        return c
+
+
+def _rows_struct(c, cfg, tensors):
+    """The fields that the norms' structs have in common, and the tensors' strides."""
+    if not 1 <= len(cfg.rows) <= 3:
+        raise ValueError("rows must have one to three dimensions")
+    pad = 3 - len(cfg.rows)
+    c.n = (ctypes.c_int32 * 3)(*([1] * pad + [_int32("rows", n) for n in cfg.rows]))
+    c.C, c.eps = _int32("C", cfg.C), _fp32("eps", cfg.eps)
+    c.dtype, c.wdtype = _dtype_code(cfg.dtype), _dtype_code(cfg.wdtype)
+    for name, t in tensors.items():
+        s = [0] * pad + _row_strides(t)
+        if any(s):
+            # dimensions in front of the rows have one entry: any distance will do
+            setattr(c, name, (ctypes.c_int64 * 3)(*[x or cfg.C for x in s[:pad]], *s[pad:]))
+    return c
 
 
 def _int32(name: str, value) -> int:
@@ -780,6 +901,144 @@ def norm_backward(cfg: NormConfig, x, mean, rstd, dy, w=None, dx=None, dw=None, 
     _call(plan, lib.mita_norm_backward, (x.data_ptr(), _ptr(w), mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(),
                                          _ptr(dx), _ptr(dw), _ptr(db), wp, wn), stream)
     return dx, dw, db
+
+
+def rms_check(cfg: RmsConfig) -> int:
+    return load_library().mita_rms_check(ctypes.byref(cfg.struct()))
+
+
+def rms_workspace_size(cfg: RmsConfig) -> int:
+    """Bytes of workspace rms_backward needs for the weight's gradient."""
+    return int(load_library().mita_rms_workspace_size(ctypes.byref(cfg.struct())))
+
+
+def _rms_forward_plan(cfg, x, w, res, h, y, scales, rstd):
+    dt, wt = cfg.torch_dtype, cfg.torch_wdtype
+    _tensor(x, "x", cfg.shape, dt, None)
+    dev = x.device
+    if w is not None:
+        _packed(w, "w", (cfg.C,), wt, dev)
+    for t, name in ((res, "res"), (h, "h")):
+        if t is not None:
+            _tensor(t, name, cfg.shape, dt, dev)
+    if y is not None:
+        _tensor(y, "y", cfg.shape, cfg.torch_ydtype, dev)
+    if scales is not None:
+        if cfg.out != "e4m3":
+            raise ValueError("scales come with out = 'e4m3' only")
+        _packed(scales, "scales", cfg.scales_shape, torch.float32, dev)
+    if rstd is not None:
+        _packed(rstd, "rstd", cfg.rows, torch.float32, dev)
+    rows = _like(x)
+    outs = (rows[:2] + (cfg.torch_ydtype,), rows, _dense(cfg.scales_shape, torch.float32),
+            _dense(cfg.rows, torch.float32))
+    given = {n: t for n, t in (("x", x), ("res", res)) if t is not None}
+    return _Plan(cfg.struct(h=_place(h, outs[1]), y=_place(y, outs[0]), **given), 0, dev, outs)
+
+
+def rms_forward(cfg: RmsConfig, x, w=None, res=None, h=None, y=None, scales=None, rstd=None, want_h=True,
+                want_rstd=True, stream=None):
+    """RMS norm of x + res (mita_rms_forward): (y like x, its scales or None, the
+    sum h or None without a residual, rstd [rows] fp32 or None). x and res may be
+    strided (their last dimension dense)."""
+    lib = load_library()
+    plan = _plan_for(cfg, "forward", (x, w, res, h, y, scales, rstd), _rms_forward_plan)
+    with _NOW if stream is None else _on(plan, stream):
+        y = plan.out(y, 0)
+        if h is None and res is not None and want_h:
+            h = plan.new(1)
+        if cfg.out == "e4m3":
+            scales = plan.out(scales, 2)
+        if want_rstd:
+            rstd = plan.out(rstd, 3)
+    _call(plan, lib.mita_rms_forward, (x.data_ptr(), _ptr(res), _ptr(w), _ptr(h), y.data_ptr(), _ptr(scales),
+                                       _ptr(rstd)), stream)
+    return y, scales, h, rstd
+
+
+def _rms_backward_plan(cfg, h, rstd, dy, w, dh, dx, dw):
+    dt, wt = cfg.torch_dtype, cfg.torch_wdtype
+    _tensor(h, "h", cfg.shape, dt, None)
+    dev = h.device
+    _tensor(dy, "dy", cfg.shape, dt, dev)
+    _packed(rstd, "rstd", cfg.rows, torch.float32, dev)
+    for t, name in ((dh, "dh"), (dx, "dx")):
+        if t is not None:
+            _tensor(t, name, cfg.shape, dt, dev)
+    for t, name in ((w, "w"), (dw, "dw")):
+        if t is not None:
+            _packed(t, name, (cfg.C,), wt, dev)
+    outs = (_like(h), _dense((cfg.C,), wt))
+    given = {} if dh is None else {"dh": dh}
+    c = cfg.struct(h=h, dy=dy, dx=_place(dx, outs[0]), **given)
+    return _Plan(c, int(load_library().mita_rms_workspace_size(ctypes.byref(c))), dev, outs)
+
+
+def rms_backward(cfg: RmsConfig, h, rstd, dy, w=None, dh=None, dx=None, dw=None, want_dx=True, want_weight=True,
+                 ws=None, stream=None):
+    """Gradients (dx, dw) of rms_forward (mita_rms_backward) from those of y (dy)
+    and of h (dh, or None); dx is x's and the residual's alike. Either is None unless
+    wanted."""
+    lib = load_library()
+    plan = _plan_for(cfg, "backward", (h, rstd, dy, w, dh, dx, dw), _rms_backward_plan)
+    with _NOW if stream is None else _on(plan, stream):
+        if want_dx:
+            dx = plan.out(dx, 0)
+        if want_weight:
+            dw = plan.out(dw, 1)
+        ws, wp, wn = _ws_for(plan, ws) if dw is not None else (None, None, 0)
+    _call(plan, lib.mita_rms_backward, (h.data_ptr(), _ptr(w), rstd.data_ptr(), dy.data_ptr(), _ptr(dh), _ptr(dx),
+                                        _ptr(dw), wp, wn), stream)
+    return dx, dw
+
+
+def rope_check(cfg: RopeConfig) -> int:
+    return load_library().mita_rope_check(ctypes.byref(cfg.struct()))
+
+
+def _rope_plan(cfg, q, k, pos, qo, ko):
+    _tensor(q, "q", cfg.q_shape, cfg.torch_dtype, None)
+    dev = q.device
+    if qo is not None:
+        _tensor(qo, "qo", cfg.q_shape, cfg.torch_dtype, dev)
+    if k is None and ko is not None:
+        raise ValueError("ko is given without k")
+    for t, name in ((k, "k"), (ko, "ko")):
+        if t is not None:
+            _tensor(t, name, cfg.k_shape, cfg.torch_dtype, dev)
+    pos_b = 0
+    if pos is not None:
+        per = isinstance(pos, torch.Tensor) and pos.dim() == 2
+        _packed(pos, "pos", (cfg.B, cfg.N) if per else (cfg.N,), torch.int32, dev)
+        pos_b = cfg.N if per else 0
+    outs = (_like(q), None if k is None else _like(k))
+    given = {"q": q, "qo": _place(qo, outs[0])}
+    if k is not None:
+        given.update(k=k, ko=_place(ko, outs[1]))
+    return _Plan(cfg.struct(pos_b, **given), 0, dev, outs)
+
+
+def _rope(fn, cfg, q, k, pos, qo, ko, stream):
+    plan = _plan_for(cfg, "rope", (q, k, pos, qo, ko), _rope_plan)
+    with _NOW if stream is None else _on(plan, stream):
+        qo = plan.out(qo, 0)
+        if k is not None:
+            ko = plan.out(ko, 1)
+    _call(plan, fn, (q.data_ptr(), _ptr(k), _ptr(pos), qo.data_ptr(), _ptr(ko)), stream)
+    return qo, ko
+
+
+def rope_forward(cfg: RopeConfig, q, k=None, pos=None, qo=None, ko=None, stream=None):
+    """Rotary positions (mita_rope_forward): (qo like q, ko like k or None). pos:
+    [N] or [B, N] int32 device tensor, or None for cfg.first, cfg.first + 1, ..; q
+    and k may be strided (their last dimension dense), qo may be q and ko k."""
+    return _rope(load_library().mita_rope_forward, cfg, q, k, pos, qo, ko, stream)
+
+
+def rope_backward(cfg: RopeConfig, dqo, dko=None, pos=None, dq=None, dk=None, stream=None):
+    """Gradients (dq, dk) of rope_forward's inputs from those of its outputs
+    (mita_rope_backward)."""
+    return _rope(load_library().mita_rope_backward, cfg, dqo, dko, pos, dq, dk, stream)
 
 
 class Timer:
