@@ -583,6 +583,49 @@ int mita_rope_backward(const mita_rope_cfg_t *cfg, const void *dqo, const void *
                        void *dk, mita_stream_t stream);
 
 /*
+ * Dense attention of a batch whose sequences share prefixes. B / Bp consecutive
+ * sequences share a prefix: sequence b's keys are the p_len keys of prefix
+ * b / (B / Bp), then its own k_len, as if they stood in one tensor. Query i has
+ * position p_len + k_len - q_len + i there, and sees the positions from p - left
+ * to p + right, as in mita_dense_cfg_t.
+ */
+typedef struct {
+  int32_t B, Bp;           /* sequences, prefixes; Bp divides B */
+  int32_t H, H_kv;         /* query heads (at most 4096), key/value heads; H_kv divides H */
+  int32_t N;               /* queries of a sequence, in [1, MITA_DENSE_MAX_N]; B / Bp * N * H / H_kv at most 2^27 */
+  int32_t P, N_k;          /* keys of a prefix, in [1, MITA_DENSE_MAX_N], and of a sequence, in [0, MITA_DENSE_MAX_N] */
+  int32_t d;               /* 64 or 128 */
+  int32_t dtype;           /* MITA_F32 or MITA_BF16: storage of all tensors but the log-sum-exps */
+  int32_t left, right;     /* window, -1 for no bound */
+  float scale;             /* softmax scale; 0 means 1/sqrt(d) */
+  mita_strides_t q, kp, vp, k, v, o;  /* as in mita_dense_cfg_t */
+} mita_prefix_cfg_t;
+
+/* Host-only validation of cfg; a status code. */
+int mita_prefix_check(const mita_prefix_cfg_t *cfg);
+
+/* Bytes of workspace mita_prefix_forward needs (0 if cfg is invalid). It depends
+ * on the sizes, the type and the window, not on the strides. */
+size_t mita_prefix_workspace_size(const mita_prefix_cfg_t *cfg);
+
+/*
+ * o and lse as mita_dense_forward's over each sequence's prefix and own keys, with
+ * its conventions for scores, roundings, values out of range and rows without keys.
+ *   q, o : [B, H, N, d];  kp, vp : [Bp, H_kv, P, d];  k, v : [B, H_kv, N_k, d], or
+ *          NULL with N_k = 0; o must not overlap an input;
+ *   q_len, k_len : [B], p_len : [Bp] int32 lengths, or NULL (clamped as there);
+ *   lse  : [B, H, N] fp32 contiguous output, or NULL;
+ *   ws   : >= mita_prefix_workspace_size(cfg) bytes.
+ * A prefix is read once for all rows of its sequences where these are few (single
+ * tokens), and their parts are joined with those of their own keys in a fixed order:
+ * results are the same bit for bit from call to call. Serving alone: there is no
+ * backward pass (mita_dense_backward takes the keys in one tensor).
+ */
+int mita_prefix_forward(const mita_prefix_cfg_t *cfg, const void *q, const void *kp, const void *vp, const void *k,
+                        const void *v, const int32_t *q_len, const int32_t *p_len, const int32_t *k_len, void *o,
+                        float *lse, void *ws, size_t ws_bytes, mita_stream_t stream);
+
+/*
  * Per-launch timing of mita_forward with HIP events (profiling aid).
  * A timer holds event slots for up to max_calls forward calls. Each
  * mita_forward_timed call records one event on the stream before its first

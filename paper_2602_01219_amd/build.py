@@ -25,7 +25,8 @@ LIB = os.path.join(PKG, "libmita.so")
 ARCH = "gfx950"
 
 SOURCES = ["mita_api.hip", "pool_scores.hip", "topk.hip", "select.hip", "route_attend.hip", "backward.hip", "tome.hip",
-           "dense_forward.hip", "dense_backward.hip", "norm.hip", "rms.hip", "rope.hip"]
+           "dense_forward.hip", "dense_backward.hip", "dense_prefix.hip", "norm.hip", "rms.hip",
+           "rope.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 OBJDUMP = os.environ.get("LLVM_OBJDUMP", "/opt/rocm/llvm/bin/llvm-objdump")

@@ -229,4 +229,9 @@ hipError_t launch_rms_backward(const mita_rms_cfg_t &c, const void *h, const voi
 hipError_t launch_rope(const mita_rope_cfg_t &c, const void *q, const void *k, const int32_t *pos, void *qo, void *ko,
                        bool back, hipStream_t st);
 
+// Dense attention over shared prefixes (mita_prefix_forward).
+hipError_t launch_prefix_forward(const mita_prefix_cfg_t &c, const void *q, const void *kp, const void *vp,
+                                 const void *k, const void *v, const int32_t *q_len, const int32_t *p_len,
+                                 const int32_t *k_len, void *o, float *lse, void *ws, hipStream_t st);
+
 }  // namespace mita

@@ -523,4 +523,129 @@ inline void rope_turns(const mita_rope_cfg_t &c, double *f) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// Dense attention over shared prefixes
+// ---------------------------------------------------------------------------
+inline size_t elem_bytes(const mita_prefix_cfg_t &c) { return c.dtype == MITA_F32 ? 4 : 2; }
+inline float eff_scale(const mita_prefix_cfg_t &c) { return c.scale != 0.f ? c.scale : 1.0f / std::sqrt((float)c.d); }
+inline int group(const mita_prefix_cfg_t &c) { return c.H / c.H_kv; }
+// Rows that read the same keys: of a sequence (its own keys), and of the sequences
+// that share a prefix.
+inline int64_t dense_rows(const mita_prefix_cfg_t &c) { return (int64_t)c.N * group(c); }
+inline int64_t shared_rows(const mita_prefix_cfg_t &c) { return dense_rows(c) * (c.B / c.Bp); }
+inline int64_t slices(const mita_prefix_cfg_t &c) { return (int64_t)c.B * c.H_kv; }
+inline Strided strided(int64_t b, int64_t h, int64_t n, int64_t d, const mita_strides_t &s0) {
+  const mita_strides_t s = strides_or(s0, h, n, d);
+  return Strided{{b, h, n}, {s.b, s.h, s.n}, d};
+}
+inline Strided strided_q(const mita_prefix_cfg_t &c, const mita_strides_t &s) { return strided(c.B, c.H, c.N, c.d, s); }
+inline Strided strided_p(const mita_prefix_cfg_t &c, const mita_strides_t &s) { return strided(c.Bp, c.H_kv, c.P, c.d, s); }
+inline Strided strided_k(const mita_prefix_cfg_t &c, const mita_strides_t &s) {
+  return strided(c.B, c.H_kv, std::max(1, c.N_k), c.d, s);
+}
+
+inline int check_prefix(const mita_prefix_cfg_t *c, std::string *err) {
+  auto fail = [&](int st, const std::string &msg) {
+    if (err) *err = msg;
+    return st;
+  };
+  if (!c) return fail(MITA_ERR_INVALID_ARG, "cfg is NULL");
+  if (c->B < 1 || c->Bp < 1 || c->H < 1 || c->H_kv < 1 || c->N < 1 || c->P < 1 || c->N_k < 0 || c->d < 1)
+    return fail(MITA_ERR_INVALID_ARG, "B, Bp, H, H_kv, N, P, d must be >= 1 and N_k >= 0");
+  if (c->B % c->Bp != 0) return fail(MITA_ERR_INVALID_ARG, "Bp must divide B");
+  if (c->H % c->H_kv != 0) return fail(MITA_ERR_INVALID_ARG, "H_kv must divide H");
+  if (c->dtype != MITA_F32 && c->dtype != MITA_BF16)
+    return fail(MITA_ERR_UNSUPPORTED, "dtype must be MITA_F32 or MITA_BF16");
+  if (c->d != 64 && c->d != 128) return fail(MITA_ERR_UNSUPPORTED, "d must be 64 or 128");
+  if (c->N > MITA_DENSE_MAX_N || c->P > MITA_DENSE_MAX_N || c->N_k > MITA_DENSE_MAX_N)
+    return fail(MITA_ERR_UNSUPPORTED, "N, P and N_k must not exceed MITA_DENSE_MAX_N");
+  if (c->left < -1 || c->right < -1) return fail(MITA_ERR_INVALID_ARG, "left and right must be >= -1");
+  if (!(c->scale >= 0.f) || std::isinf(c->scale)) return fail(MITA_ERR_INVALID_ARG, "scale must be finite and >= 0");
+  if (c->H > 4096) return fail(MITA_ERR_UNSUPPORTED, "H must not exceed 4096");
+  // row numbers are 32-bit, and so are the grids (workgroups of 256 threads, of which a
+  // launch has less than 2^32)
+  if (shared_rows(*c) > (1 << 27)) return fail(MITA_ERR_UNSUPPORTED, "B / Bp * N * (H / H_kv) must not exceed 2^27");
+  if (slices(*c) * ((dense_rows(*c) + 31) / 32) >= (1 << 23))
+    return fail(MITA_ERR_UNSUPPORTED, "too many heads and tokens for one launch");
+  const int64_t unit = 16 / (int64_t)elem_bytes(*c);
+  const struct {
+    const char *name;
+    Strided x;
+    bool out;
+  } all[6] = {{"q", strided_q(*c, c->q), false}, {"kp", strided_p(*c, c->kp), false}, {"vp", strided_p(*c, c->vp), false},
+              {"k", strided_k(*c, c->k), false}, {"v", strided_k(*c, c->v), false},   {"o", strided_q(*c, c->o), true}};
+  for (const auto &t : all) {
+    for (int i = 0; i < 3; ++i) {
+      if (t.x.s[i] < 0 || t.x.s[i] > (int64_t)1 << 40)
+        return fail(MITA_ERR_INVALID_ARG, std::string("strides of ") + t.name + " must be in [0, 2^40]");
+      if (t.x.n[i] > 1 && t.x.s[i] % unit != 0)
+        return fail(MITA_ERR_INVALID_ARG, std::string("strides of ") + t.name + " must be multiples of 16 bytes");
+    }
+    if (t.x.n[2] > 1 && (t.x.s[2] < c->d || t.x.s[2] > MITA_DENSE_MAX_STRIDE))
+      return fail(MITA_ERR_INVALID_ARG,
+                  std::string("token stride of ") + t.name + " must be in [d, MITA_DENSE_MAX_STRIDE]");
+    if (t.out && !nested(t.x))
+      return fail(MITA_ERR_INVALID_ARG, std::string("strides of ") + t.name + " give elements the same address");
+  }
+  return MITA_OK;
+}
+
+// Launch plan. `shared`: a prefix's keys are taken by the rows of all its sequences
+// together, each sequence's own keys by its rows, and the parts are joined; else every
+// row tile of a sequence goes through the prefix's keys and then its own.
+constexpr int PREFIX_MAX_SPLITS = 64;
+struct PrefixPlan {
+  bool shared;
+  bool few;           // DENSE_FEW rows per workgroup, else DENSE_TQ (shared: of the prefix's part; DENSE_FEW of the other)
+  int tiles, splits;  // row tiles of a slice (shared: of a prefix's rows), key splits of each
+  int otiles, osplits;  // shared: of a sequence's own part (0 without own keys)
+  int64_t blocks, oblocks;  // workgroups
+  int slots;          // parts of a row's result; 1: none is kept
+};
+inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
+  PrefixPlan p{};
+  const int64_t rows = dense_rows(c), S = c.B / c.Bp;
+  p.shared = S > 1 && rows < DENSE_TQ;
+  if (p.shared) {
+    const int64_t prefixes = (int64_t)c.Bp * c.H_kv, all = shared_rows(c);
+    p.few = all <= DENSE_FEW;
+    p.tiles = (int)((all + (p.few ? DENSE_FEW : DENSE_TQ) - 1) / (p.few ? DENSE_FEW : DENSE_TQ));
+    const int64_t blocks = prefixes * p.tiles;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({2 * CUS / blocks, c.P / 256, PREFIX_MAX_SPLITS}));
+    p.blocks = blocks * p.splits;
+    if (c.N_k) {
+      p.otiles = (int)((rows + DENSE_FEW - 1) / DENSE_FEW);
+      const int64_t own = slices(c) * p.otiles;
+      p.osplits = (int)std::max<int64_t>(1, std::min<int64_t>({2 * CUS / own, c.N_k / 512, PREFIX_MAX_SPLITS}));
+      p.oblocks = own * p.osplits;
+    }
+    p.slots = p.splits + p.osplits;
+    return p;
+  }
+  p.tiles = (int)((rows + DENSE_TQ - 1) / DENSE_TQ);
+  p.few = rows <= DENSE_FEW || slices(c) * p.tiles < CUS;
+  if (p.few) p.tiles = (int)((rows + DENSE_FEW - 1) / DENSE_FEW);
+  const int64_t blocks = slices(c) * p.tiles, least = !p.few ? 512 : rows <= DENSE_FEW ? 256 : 1024;
+  p.splits = (int)std::max<int64_t>(
+      1, std::min<int64_t>({2 * CUS / blocks, ((int64_t)c.P + c.N_k) / least, PREFIX_MAX_SPLITS}));
+  p.blocks = blocks * p.splits;
+  p.slots = p.splits;
+  return p;
+}
+struct PrefixLayout {
+  size_t part_o, part_lse, total;  // per row and slot: normalised output and log2-sum-exp
+};
+inline PrefixLayout prefix_layout(const mita_prefix_cfg_t &c) {
+  PrefixLayout L{};
+  const PrefixPlan p = prefix_plan(c);
+  if (p.slots == 1) return L;
+  const size_t parts = (size_t)slices(c) * dense_rows(c) * p.slots;
+  L.part_lse = align_up(parts * c.d * sizeof(float));
+  L.total = L.part_lse + align_up(parts * sizeof(float));
+  return L;
+}
+inline size_t prefix_workspace_size(const mita_prefix_cfg_t *c) {
+  return check_prefix(c, nullptr) != MITA_OK ? 0 : prefix_layout(*c).total;
+}
+
 }  // namespace mita

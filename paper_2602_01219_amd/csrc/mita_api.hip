@@ -388,6 +388,11 @@ int validate(const mita_rope_cfg_t *c) {
   const int st = check_rope(c, &msg);
   return st == MITA_OK ? st : set_err(st, msg);
 }
+int validate(const mita_prefix_cfg_t *c) {
+  std::string msg;
+  const int st = check_prefix(c, &msg);
+  return st == MITA_OK ? st : set_err(st, msg);
+}
 
 int need_bytes(size_t need, const void *ws, size_t ws_bytes) {
   if (need == 0) return MITA_OK;
@@ -919,6 +924,47 @@ int mita_rope_forward(const mita_rope_cfg_t *cfg, const void *q, const void *k, 
 int mita_rope_backward(const mita_rope_cfg_t *cfg, const void *dqo, const void *dko, const int32_t *pos, void *dq,
                        void *dk, mita_stream_t stream) {
   return guarded([&]() -> int { return rope(cfg, dqo, dko, pos, dq, dk, true, (hipStream_t)stream); });
+}
+
+int mita_prefix_check(const mita_prefix_cfg_t *cfg) {
+  return guarded([&]() -> int { return validate(cfg); });
+}
+
+size_t mita_prefix_workspace_size(const mita_prefix_cfg_t *cfg) {
+  return guarded_size([&]() -> size_t { return prefix_workspace_size(cfg); });
+}
+
+int mita_prefix_forward(const mita_prefix_cfg_t *cfg, const void *q, const void *kp, const void *vp, const void *k,
+                        const void *v, const int32_t *q_len, const int32_t *p_len, const int32_t *k_len, void *o,
+                        float *lse, void *ws, size_t ws_bytes, mita_stream_t stream) {
+  return guarded([&]() -> int {
+    TRY(validate(cfg));
+    TRY(need_ptr(q, "q"));
+    TRY(need_ptr(kp, "kp"));
+    TRY(need_ptr(vp, "vp"));
+    TRY(need_ptr(o, "o"));
+    if (cfg->N_k) {
+      TRY(need_ptr(k, "k"));
+      TRY(need_ptr(v, "v"));
+    } else {
+      k = v = nullptr;
+    }
+    if (q_len) TRY(need_elem_ptr(q_len, 4, "q_len"));
+    if (p_len) TRY(need_elem_ptr(p_len, 4, "p_len"));
+    if (k_len) TRY(need_elem_ptr(k_len, 4, "k_len"));
+    if (lse) TRY(need_elem_ptr(lse, 4, "lse"));
+    const size_t need = prefix_workspace_size(cfg), e = elem_bytes(*cfg);
+    TRY(need_bytes(need, ws, ws_bytes));
+    const Buffer bq{"q", q, strided_q(*cfg, cfg->q), e}, bo{"o", o, strided_q(*cfg, cfg->o), e};
+    const Buffer bkp{"kp", kp, strided_p(*cfg, cfg->kp), e}, bvp{"vp", vp, strided_p(*cfg, cfg->vp), e};
+    const Buffer bk{"k", k, strided_k(*cfg, cfg->k), e}, bv{"v", v, strided_k(*cfg, cfg->v), e};
+    TRY(apart({bo, bytes_of("lse", lse, (size_t)cfg->B * cfg->H * cfg->N * 4), bytes_of("ws", need ? ws : nullptr, need)},
+              {bq, bkp, bvp, bk, bv, bytes_of("q_len", q_len, (size_t)cfg->B * 4),
+               bytes_of("p_len", p_len, (size_t)cfg->Bp * 4), bytes_of("k_len", k_len, (size_t)cfg->B * 4)}));
+    return hip_status(
+        launch_prefix_forward(*cfg, q, kp, vp, k, v, q_len, p_len, k_len, o, lse, ws, (hipStream_t)stream),
+        "prefix forward");
+  });
 }
 
 int mita_timer_create(mita_timer_t **timer, int max_calls) {

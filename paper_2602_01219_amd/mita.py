@@ -44,7 +44,8 @@ EXPORTED = ("mita_check", "mita_workspace_size", "mita_status_string", "mita_las
             "mita_dense_check", "mita_dense_workspace_size", "mita_dense_forward", "mita_dense_backward",
             "mita_norm_check", "mita_norm_workspace_size", "mita_norm_forward", "mita_norm_backward",
             "mita_rms_check", "mita_rms_workspace_size", "mita_rms_forward", "mita_rms_backward",
-            "mita_rope_check", "mita_rope_forward", "mita_rope_backward")
+            "mita_rope_check", "mita_rope_forward", "mita_rope_backward",
+            "mita_prefix_check", "mita_prefix_workspace_size", "mita_prefix_forward")
 
 
 class CfgStruct(ctypes.Structure):
@@ -84,6 +85,11 @@ class RopeCfgStruct(ctypes.Structure):
                 + [(n, StridesStruct) for n in ("q", "k", "qo", "ko")])
 
 
+class PrefixCfgStruct(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "Bp", "H", "H_kv", "N", "P", "N_k", "d", "dtype", "left", "right")]
+                + [("scale", ctypes.c_float)] + [(n, StridesStruct) for n in ("q", "kp", "vp", "k", "v", "o")])
+
+
 class MitaError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"mita status {status}: {msg}")
@@ -105,6 +111,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     cfgp = ctypes.POINTER(CfgStruct)
     densep, normp = ctypes.POINTER(DenseCfgStruct), ctypes.POINTER(NormCfgStruct)
     rmsp, ropep = ctypes.POINTER(RmsCfgStruct), ctypes.POINTER(RopeCfgStruct)
+    prefixp = ctypes.POINTER(PrefixCfgStruct)
     sig = {
         "mita_check": (I, [cfgp]),
         "mita_workspace_size": (Z, [cfgp, I]),
@@ -138,6 +145,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "mita_rope_check": (I, [ropep]),
         "mita_rope_forward": (I, [ropep, P, P, P, P, P, P]),
         "mita_rope_backward": (I, [ropep, P, P, P, P, P, P]),
+        "mita_prefix_check": (I, [prefixp]),
+        "mita_prefix_workspace_size": (Z, [prefixp]),
+        "mita_prefix_forward": (I, [prefixp] + [P] * 11 + [Z, P]),
         "mita_topk": (I, [cfgp, P, P, P, Z, P]),
         "mita_gather": (I, [cfgp, P, P, P, P, P, P]),
         "mita_route": (I, [cfgp, P, P, P, P, P, P, Z, P]),
@@ -573,6 +583,51 @@ class RopeConfig(_Planned):
                           float(self.fast), _fp32("scale", self.scale), pos_b, first)
         for name, t in tensors.items():
             setattr(c, name, StridesStruct(*_row_strides(t)))
+        return c
+
+
+@dataclass(frozen=True)
+class PrefixConfig(_Planned):
+    """Dense attention of B sequences, B / Bp consecutive ones of which share a
+    prefix (mita_prefix_cfg_t without the strides): a sequence's keys are its
+    prefix's, then its own. H_kv = 0 means H; N_k = 0: no keys of their own. The
+    window counts places in both together."""
+    B: int
+    H: int
+    N: int
+    P: int
+    d: int
+    Bp: int = 1
+    H_kv: int = 0
+    N_k: int = 0
+    dtype: str = "bf16"          # "f32" | "bf16"
+    left: int = -1
+    right: int = -1
+    scale: float = 0.0           # 0 -> 1/sqrt(d)
+
+    @property
+    def q_shape(self):
+        return (self.B, self.H, self.N, self.d)
+
+    @property
+    def p_shape(self):
+        return (self.Bp, self.H_kv or self.H, self.P, self.d)
+
+    @property
+    def k_shape(self):
+        return (self.B, self.H_kv or self.H, self.N_k, self.d)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == "f32" else torch.bfloat16
+
+    def struct(self, **tensors) -> PrefixCfgStruct:
+        B, Bp, H, N, P, N_k, d, left, right = (_int32(n, getattr(self, n)) for n in
+                                               ("B", "Bp", "H", "N", "P", "N_k", "d", "left", "right"))
+        c = PrefixCfgStruct(B, Bp, H, _int32("H_kv", self.H_kv) or H, N, P, N_k, d, _dtype_code(self.dtype), left,
+                            right, _fp32("scale", self.scale))
+        for name, t in tensors.items():
+            setattr(c, name, StridesStruct(*_strides(t)))
         return c
 
 
@@ -1039,6 +1094,56 @@ def rope_backward(cfg: RopeConfig, dqo, dko=None, pos=None, dq=None, dk=None, st
     """Gradients (dq, dk) of rope_forward's inputs from those of its outputs
     (mita_rope_backward)."""
     return _rope(load_library().mita_rope_backward, cfg, dqo, dko, pos, dq, dk, stream)
+
+
+def prefix_check(cfg: PrefixConfig) -> int:
+    return load_library().mita_prefix_check(ctypes.byref(cfg.struct()))
+
+
+def prefix_workspace_size(cfg: PrefixConfig) -> int:
+    return int(load_library().mita_prefix_workspace_size(ctypes.byref(cfg.struct())))
+
+
+def _prefix_plan(cfg, q, kp, vp, k, v, q_len, p_len, k_len, o, lse):
+    _tensor(q, "q", cfg.q_shape, cfg.torch_dtype, None)
+    dev = q.device
+    _tensor(kp, "kp", cfg.p_shape, cfg.torch_dtype, dev)
+    _tensor(vp, "vp", cfg.p_shape, cfg.torch_dtype, dev)
+    given = {"q": q, "kp": kp, "vp": vp}
+    if cfg.N_k:
+        _tensor(k, "k", cfg.k_shape, cfg.torch_dtype, dev)
+        _tensor(v, "v", cfg.k_shape, cfg.torch_dtype, dev)
+        given.update(k=k, v=v)
+    elif k is not None or v is not None:
+        raise ValueError("k and v are given, but N_k is 0")
+    _lengths(q_len, "q_len", cfg.B, dev)
+    _lengths(p_len, "p_len", cfg.Bp, dev)
+    _lengths(k_len, "k_len", cfg.B, dev)
+    if o is not None:
+        _tensor(o, "o", cfg.q_shape, cfg.torch_dtype, dev)
+    if lse is not None:
+        _packed(lse, "lse", cfg.q_shape[:3], torch.float32, dev)
+    outs = (_like(q), _dense(cfg.q_shape[:3], torch.float32))
+    c = cfg.struct(o=_place(o, outs[0]), **given)
+    return _Plan(c, int(load_library().mita_prefix_workspace_size(ctypes.byref(c))), dev, outs)
+
+
+def prefix_forward(cfg: PrefixConfig, q, kp, vp, k=None, v=None, q_len=None, p_len=None, k_len=None, o=None, lse=None,
+                   want_lse=True, ws=None, stream=None):
+    """Dense attention over shared prefixes kp, vp [Bp, H_kv, P, d] and each
+    sequence's own k, v [B, H_kv, N_k, d] (mita_prefix_forward): (o [B, H, N, d], lse
+    [B, H, N] fp32 or None). Tensors may be strided (their last dimension dense);
+    q_len, k_len are [B], p_len is [Bp] int32 device tensors."""
+    lib = load_library()
+    plan = _plan_for(cfg, "forward", (q, kp, vp, k, v, q_len, p_len, k_len, o, lse), _prefix_plan)
+    with _NOW if stream is None else _on(plan, stream):
+        o = plan.out(o, 0)
+        if lse is None and want_lse:
+            lse = plan.new(1)
+        ws, wp, wn = _ws_for(plan, ws)
+    _call(plan, lib.mita_prefix_forward, (q.data_ptr(), kp.data_ptr(), vp.data_ptr(), _ptr(k), _ptr(v), _ptr(q_len),
+                                          _ptr(p_len), _ptr(k_len), o.data_ptr(), _ptr(lse), wp, wn), stream)
+    return o, lse
 
 
 class Timer:
