@@ -116,33 +116,29 @@ template <int TR> struct PrefixTiles {
 // Tiles [t0, t1) in the order a workgroup takes them: those seen whole by every row
 // first, of the prefix and then the own ones, then the others.
 struct PrefixOrder {
-  int start[6], end[6], nfull, total;  // end: of the positions of segment i
+  int s0, s1, s2, s3, s4, s5, e0, e1, e2, e3, e4;  // position p of segment i (up to ei) is tile si + p
+  int nfull, total;
   template <int TR>
   __device__ __forceinline__ PrefixOrder(const PrefixTiles<TR> &x, int t0, int t1, const PrefixBounds &w) {
     // the prefix's whole tiles [a0, a1), the own ones [b0, b1), as tile numbers
     auto up = [](int y) { return y > 0 ? (y + TR - 1) / TR : 0; };
     auto down = [](int y) { return y > 0 ? y / TR : 0; };
     const int m = max(t0, min(x.np, t1));
-    int a1 = max(t0, min(down(min(w.hi0, x.pl) - x.pb), m));
+    const int a1 = max(t0, min(down(min(w.hi0, x.pl) - x.pb), m));
     const int a0 = min(max(up(w.lo1 - x.pb), t0), a1);
-    int b1 = max(m, min(x.np + down(w.hi0 - x.pl - x.ob), t1));
+    const int b1 = max(m, min(x.np + down(w.hi0 - x.pl - x.ob), t1));
     const int b0 = min(max(x.np + up(w.lo1 - x.pl - x.ob), m), b1);
-    const int s[6] = {a0, b0, t0, a1, m, b1}, n[6] = {a1 - a0, b1 - b0, a0 - t0, m - a1, b0 - m, t1 - b1};
-    int e = 0;
-#pragma unroll
-    for (int i = 0; i < 6; ++i) {
-      start[i] = s[i] - e;
-      e += max(0, n[i]);
-      end[i] = e;
-    }
-    nfull = end[1];
+    s0 = a0, e0 = a1 - a0;
+    s1 = b0 - e0, e1 = e0 + b1 - b0;
+    s2 = t0 - e1, e2 = e1 + a0 - t0;
+    s3 = a1 - e2, e3 = e2 + m - a1;
+    s4 = m - e3, e4 = e3 + b0 - m;
+    s5 = b1 - e4;
+    nfull = e1;
     total = max(0, t1 - t0);
   }
   __device__ __forceinline__ int at(int p) const {
-    int t = start[5] + p;
-#pragma unroll
-    for (int i = 4; i >= 0; --i) t = p < end[i] ? start[i] + p : t;
-    return t;
+    return p + (p < e0 ? s0 : p < e1 ? s1 : p < e2 ? s2 : p < e3 ? s3 : p < e4 ? s4 : s5);
   }
 };
 
@@ -436,33 +432,64 @@ __global__ void __launch_bounds__(256, WAY == WAY_FEW || WAY == WAY_SHARED_FEW ?
     prefix_few<T, D>(a, it, ldsK, ldsV, join.of[0], join.of[1]);
 }
 
-// Joins a row's parts by their log-sum-exps: D / 4 lanes per row.
-template <typename T, int D> __global__ void __launch_bounds__(256) prefix_join_kernel(PrefixArgs a) {
-  constexpr int L = D / 4;
-  const int64_t i = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const int c = threadIdx.x % L;
+// Joins a row's parts by their log-sum-exps. ROWS = 1: a workgroup per row, whose groups
+// of D / 4 lanes take the parts in turn and add theirs in a fixed order; else a group per
+// row.
+template <typename T, int D, int ROWS> __global__ void __launch_bounds__(256) prefix_join_kernel(PrefixArgs a) {
+  constexpr int L = D / 4, GROUPS = 256 / L;
+  static_assert(ROWS == 1 || ROWS == GROUPS, "a row per workgroup or per group");
+  __shared__ float weight[ROWS == 1 ? 2 * PREFIX_MAX_SPLITS : 1];
+  __shared__ float4 sums[ROWS == 1 ? GROUPS : 1][L];
+  const int c = threadIdx.x % L, g = threadIdx.x / L;
+  const int64_t i = ROWS == 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * ROWS + g;
   if (i >= (int64_t)a.B * a.Hkv * a.rows) return;
+  const float *lse = a.part_lse + i * a.slots;
+  const float *part = a.part_o + i * a.slots * D + 4 * c;
+  float m = -INFINITY, l = 0.f;
+  bool sees;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float f, const float4 &y) {
+    o.x = __builtin_fmaf(f, y.x, o.x);
+    o.y = __builtin_fmaf(f, y.y, o.y);
+    o.z = __builtin_fmaf(f, y.z, o.z);
+    o.w = __builtin_fmaf(f, y.w, o.w);
+  };
+  if constexpr (ROWS == 1) {
+    // every wave forms the weights of all parts, two per lane; parts that weigh nothing hold 0
+    const int lane = threadIdx.x & 63;
+    const float z0 = lane < a.slots ? lse[lane] : -INFINITY, z1 = lane + 64 < a.slots ? lse[lane + 64] : -INFINITY;
+    sees = __ballot(z0 != -INFINITY || z1 != -INFINITY) != 0;
+    m = wave_max(fmaxf(z0, z1));  // (passes over NaN, whose weight then is NaN)
+    const float f0 = z0 <= DENSE_NO_WEIGHT ? 0.f : __builtin_amdgcn_exp2f(z0 - m);
+    const float f1 = z1 <= DENSE_NO_WEIGHT ? 0.f : __builtin_amdgcn_exp2f(z1 - m);
+    l = wave_sum(f0 + f1);
+    if (threadIdx.x < 64) {
+      weight[lane] = f0;
+      weight[lane + 64] = f1;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int j = g; j < a.slots; j += GROUPS) add(weight[j], *reinterpret_cast<const float4 *>(part + j * D));
+    sums[g][c] = o;
+    __syncthreads();
+    if (g > 0) return;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) add(1.f, sums[k][c]);
+  } else {
+    sees = false;
+    for (int j = 0; j < a.slots; ++j) {
+      sees |= lse[j] != -INFINITY;
+      m = fmaxf(m, lse[j]);
+    }
+#pragma unroll 4
+    for (int j = 0; j < a.slots; ++j) {
+      const float z = lse[j], f = z <= DENSE_NO_WEIGHT ? 0.f : __builtin_amdgcn_exp2f(z - m);
+      l += f;
+      add(f, *reinterpret_cast<const float4 *>(part + j * D));
+    }
+  }
   const int s = (int)(i / a.rows), row = (int)(i - (int64_t)s * a.rows);
   const int b = s / a.Hkv, tok = div_by(a.magic, row), head = (s - b * a.Hkv) * a.G + row - tok * a.G;
-  float m = -INFINITY, l = 0.f;
-  bool sees = false;
-  for (int j = 0; j < a.slots; ++j) {
-    const float z = a.part_lse[i * a.slots + j];
-    sees |= z != -INFINITY;
-    m = fmaxf(m, z);
-  }
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j = 0; j < a.slots; ++j) {
-    const float z = a.part_lse[i * a.slots + j];
-    if (z <= DENSE_NO_WEIGHT) continue;
-    const float f = __builtin_amdgcn_exp2f(z - m);
-    const float4 y = *reinterpret_cast<const float4 *>(a.part_o + (i * a.slots + j) * D + 4 * c);
-    l += f;
-    o.x += f * y.x;
-    o.y += f * y.y;
-    o.z += f * y.z;
-    o.w += f * y.w;
-  }
   float inv, lse2;
   dense_norm(!sees, l, m, inv, lse2);
   T *out = (T *)(a.o.p + b * a.o.b + head * a.o.h + (int64_t)tok * a.o.n) + 4 * c;
@@ -485,8 +512,12 @@ template <typename T, int D> hipError_t forward_t(const PrefixArgs &a, const Pre
     prefix_kernel<T, D, WAY_TILE><<<grid, 256, 0, st>>>(a);
   const hipError_t e = launched("prefix_kernel", st);
   if (e != hipSuccess || p.slots == 1) return e;
-  const int64_t rows = (int64_t)a.B * a.Hkv * a.rows, per = 256 / (D / 4);
-  prefix_join_kernel<T, D><<<dim3((unsigned)((rows + per - 1) / per)), 256, 0, st>>>(a);
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.rows;
+  constexpr int PER = 256 / (D / 4);
+  if (p.slots > 4 && rows < (1 << 23))
+    prefix_join_kernel<T, D, 1><<<dim3((unsigned)rows), 256, 0, st>>>(a);
+  else
+    prefix_join_kernel<T, D, PER><<<dim3((unsigned)((rows + PER - 1) / PER)), 256, 0, st>>>(a);
   return launched("prefix_join_kernel", st);
 }
 

@@ -602,16 +602,43 @@ struct PrefixPlan {
   int64_t blocks, oblocks;  // workgroups
   int slots;          // parts of a row's result; 1: none is kept
 };
+// Key splits of `tiles` row tiles of DENSE_TQ rows that go through `keys` keys each. A CU
+// with n of their parts takes, per key, `alone` ns for one and `pair` for each of more,
+// which share it two at a time (measured with 16000 keys: 256 tiles 281 us, 416 tiles 413
+// in bf16, d = 128), a part about 150 keys more to begin and end, the join 10 TB/s and a
+// launch. 416 tiles of 8518 keys: 214 us whole, 214, 192, 199 and 239 in two to five parts;
+// 208 of 16000: 281, 227, 248, 241; 96 of 16000: 282, 152, 147, 124, and 126 in eight.
+inline int prefix_splits(const mita_prefix_cfg_t &c, int64_t tiles, int64_t keys) {
+  const bool f32 = c.dtype == MITA_F32, wide = c.d == 128;
+  const double alone = f32 ? (wide ? 93 : 50) : wide ? 17.5 : 14.7, pair = f32 ? alone : wide ? 12.8 : 8.7;
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 16 && (s == 1 || keys / s >= 256); ++s) {
+    const int64_t n = (tiles * s + CUS - 1) / CUS;
+    double t = (n == 1 ? alone : (double)n * pair) * ((double)keys / s + 150);
+    if (s > 1) t += (double)slices(c) * dense_rows(c) * s * c.d * 8e-4 + 3000;
+    if (s == 1 || t < least) best = s, least = t;
+  }
+  return best;
+}
 inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
   PrefixPlan p{};
-  const int64_t rows = dense_rows(c), S = c.B / c.Bp;
-  p.shared = S > 1 && rows < DENSE_TQ;
+  const int64_t rows = dense_rows(c), S = c.B / c.Bp, keys = (int64_t)c.P + c.N_k;
+  // Together and apart, us, bf16, d = 128, 8 key heads: 1 row of 64 sequences, 1000 prefix
+  // keys 21 and 21, 4000 24 and 51; 4 rows of 16, 500 keys 12 and 13, 2000 15 and 18, 8000 19
+  // and 35; 8 rows of 16, 1000 keys 16 and 15, 2000 17 and 18; 16 rows of 16, 2000 keys 20
+  // and 19, 8000 28 and 35; 32 rows of 16, 8000 keys 39 and 37. Short prefixes have no
+  // splits to join apart (250 keys, 4 rows of 4: 12 and 10).
+  p.shared = S > 1 && rows < DENSE_FEW && c.P >= std::max<int64_t>(1024, 200 * rows);
   if (p.shared) {
     const int64_t prefixes = (int64_t)c.Bp * c.H_kv, all = shared_rows(c);
     p.few = all <= DENSE_FEW;
     p.tiles = (int)((all + (p.few ? DENSE_FEW : DENSE_TQ) - 1) / (p.few ? DENSE_FEW : DENSE_TQ));
     const int64_t blocks = prefixes * p.tiles;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({2 * CUS / blocks, c.P / 256, PREFIX_MAX_SPLITS}));
+    // one workgroup per CU, beside which others take the own keys: a part of 128 rows is
+    // 64 KB to write and read again (128 rows of 32768 keys and 8 key heads, each of 32
+    // sequences up to 1024 of its own, d = 128: 61 us with 32 splits, 71 with 16, 72 with 64)
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({CUS / blocks, c.P / 128, PREFIX_MAX_SPLITS}));
     p.blocks = blocks * p.splits;
     if (c.N_k) {
       p.otiles = (int)((rows + DENSE_FEW - 1) / DENSE_FEW);
@@ -622,13 +649,19 @@ inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
     p.slots = p.splits + p.osplits;
     return p;
   }
+  // Rows by 32 and by 128, us, bf16, d = 128: 96 tiles of 128 rows and 1000 keys 17 and 25,
+  // 4000 46 and 45, 16000 157 and 124; 208 tiles and 1000 keys 21 and 27, 4000 76 and 66; d =
+  // 64: 96 tiles and 4000 keys 31 and 33, 16000 105 and 80; 208 tiles and 4000 43 and 45.
   p.tiles = (int)((rows + DENSE_TQ - 1) / DENSE_TQ);
-  p.few = rows <= DENSE_FEW || slices(c) * p.tiles < CUS;
-  if (p.few) p.tiles = (int)((rows + DENSE_FEW - 1) / DENSE_FEW);
-  const int64_t blocks = slices(c) * p.tiles, least = !p.few ? 512 : rows <= DENSE_FEW ? 256 : 1024;
-  p.splits = (int)std::max<int64_t>(
-      1, std::min<int64_t>({2 * CUS / blocks, ((int64_t)c.P + c.N_k) / least, PREFIX_MAX_SPLITS}));
-  p.blocks = blocks * p.splits;
+  p.few = rows <= 64 || slices(c) * p.tiles * keys * (c.d / 64) < 1000000;
+  if (p.few) {
+    p.tiles = (int)((rows + DENSE_FEW - 1) / DENSE_FEW);
+    const int64_t blocks = slices(c) * p.tiles, least = rows <= DENSE_FEW ? 256 : 1024;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({2 * CUS / blocks, keys / least, PREFIX_MAX_SPLITS}));
+  } else {
+    p.splits = prefix_splits(c, slices(c) * p.tiles, keys);
+  }
+  p.blocks = slices(c) * p.tiles * p.splits;
   p.slots = p.splits;
   return p;
 }

@@ -82,6 +82,7 @@ def test_against_float64(case, d, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_scores_move_the_reference(dtype):
     # scores of standard deviation 25: the parts' maxima lie far apart, most weights vanish
+    run_case(mita.PrefixConfig(12, 4, 1, 1900, 64, H_kv=2, N_k=300, dtype=dtype, right=0), std=25.0)
     run_case(mita.PrefixConfig(12, 4, 1, 900, 64, H_kv=2, N_k=300, dtype=dtype, right=0), std=25.0)
     run_case(mita.PrefixConfig(2, 4, 150, 300, 64, H_kv=2, N_k=150, dtype=dtype, right=0, scale=0.9), std=6.0)
 
@@ -112,10 +113,10 @@ def test_lengths_past_the_sizes_are_clamped():
     assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
-@pytest.mark.parametrize("N", [1, 140])
-def test_values_out_of_range(N):
+@pytest.mark.parametrize("N,P", [(1, 300), (1, 1300), (140, 300)])
+def test_values_out_of_range(N, P):
     # a NaN or a score past the range makes its row NaN, and that alone
-    cfg = mita.PrefixConfig(6, 2, N, 300, 64, N_k=200, dtype="f32", right=0)
+    cfg = mita.PrefixConfig(6, 2, N, P, 64, N_k=200, dtype="f32", right=0)
     q, kp, vp, k, v = make(cfg, "bhnd", 4)
     ok = mita.prefix_forward(cfg, q, kp, vp, k, v)
     q[1, 1, 0, 5] = float("nan")
@@ -128,10 +129,10 @@ def test_values_out_of_range(N):
     assert torch.equal(o[keep], ok[0][keep]) and torch.equal(lse[keep], ok[1][keep])
 
 
-@pytest.mark.parametrize("N", [1, 140])
-def test_parts_without_weight(N):
+@pytest.mark.parametrize("N,P", [(1, 600), (1, 1600), (140, 600)])
+def test_parts_without_weight(N, P):
     # scores so low in the prefix that they weigh nothing beside the own keys', and the other way round
-    cfg = mita.PrefixConfig(6, 2, N, 600, 64, N_k=200, dtype="f32")
+    cfg = mita.PrefixConfig(6, 2, N, P, 64, N_k=200, dtype="f32")
     for low in ("prefix", "own"):
         q, kp, vp, k, v = make(cfg, "bhnd", 5)
         q[..., 0] = 1.0
@@ -241,6 +242,8 @@ def test_refusals():
         with pytest.raises(mita.MitaError) as e:
             mita.prefix_forward(cfg, q, kp, vp, k, v, **kw)
         assert e.value.status == mita.MITA_ERR_INVALID_ARG
+    cfg = mita.PrefixConfig(4, 2, 1, 2000, 64, Bp=2, N_k=8)
+    q, kp, vp, k, v = make(cfg, "bhnd", 15)
     assert mita.prefix_workspace_size(cfg) > 0
     with pytest.raises(mita.MitaError) as e:
         mita.prefix_forward(cfg, q, kp, vp, k, v, ws=torch.empty(64, dtype=torch.uint8, device="cuda"))
