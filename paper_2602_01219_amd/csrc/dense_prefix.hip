@@ -441,7 +441,7 @@ template <typename T, int D, int ROWS> __global__ void __launch_bounds__(256) pr
   __shared__ float weight[ROWS == 1 ? 2 * PREFIX_MAX_SPLITS : 1];
   __shared__ float4 sums[ROWS == 1 ? GROUPS : 1][L];
   const int c = threadIdx.x % L, g = threadIdx.x / L;
-  const int64_t i = ROWS == 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * ROWS + g;
+  const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, i = ROWS == 1 ? block : block * ROWS + g;
   if (i >= (int64_t)a.B * a.Hkv * a.rows) return;
   const float *lse = a.part_lse + i * a.slots;
   const float *part = a.part_o + i * a.slots * D + 4 * c;
@@ -514,10 +514,15 @@ template <typename T, int D> hipError_t forward_t(const PrefixArgs &a, const Pre
   if (e != hipSuccess || p.slots == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.rows;
   constexpr int PER = 256 / (D / 4);
-  if (p.slots > 4 && rows < (1 << 23))
-    prefix_join_kernel<T, D, 1><<<dim3((unsigned)rows), 256, 0, st>>>(a);
+  // (a dimension of a launch has less than 2^32 threads)
+  auto grid2 = [](int64_t blocks) {
+    constexpr int64_t X = 1 << 20;
+    return dim3((unsigned)std::min(blocks, X), (unsigned)((blocks + X - 1) / X));
+  };
+  if (p.slots > 4)
+    prefix_join_kernel<T, D, 1><<<grid2(rows), 256, 0, st>>>(a);
   else
-    prefix_join_kernel<T, D, PER><<<dim3((unsigned)((rows + PER - 1) / PER)), 256, 0, st>>>(a);
+    prefix_join_kernel<T, D, PER><<<grid2((rows + PER - 1) / PER), 256, 0, st>>>(a);
   return launched("prefix_join_kernel", st);
 }
 

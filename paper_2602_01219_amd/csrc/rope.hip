@@ -90,6 +90,13 @@ template <typename T, int V> __device__ __forceinline__ void put(char *p, const 
   }
 }
 
+// The same elements as they are.
+template <int BYTES> struct Bits;
+template <> struct Bits<16> { using type = uint4; };
+template <> struct Bits<8> { using type = uint2; };
+template <> struct Bits<4> { using type = uint32_t; };
+template <> struct Bits<2> { using type = uint16_t; };
+
 __device__ __forceinline__ void turn(float &u, float &v, float sn, float cs) {
   const float y = u, z = v;
   u = __builtin_fmaf(y, cs, -(z * sn));
@@ -159,15 +166,16 @@ template <typename T, int V, bool IL> __global__ void __launch_bounds__(256) rop
         if constexpr (second) put<T, V>(dst + apart, v[i]);
       }
     } else {
-      float u[U][V];
+      using B = typename Bits<V * (int)sizeof(T)>::type;
+      B u[U];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         places(h + i, src, dst);
-        get<T, V>(src, u[i]);
+        u[i] = *reinterpret_cast<const B *>(src);
       }
 #pragma unroll
       for (int i = 0; i < U; ++i)
-        if (!places(h + i, src, dst)) put<T, V>(dst, u[i]);
+        if (!places(h + i, src, dst)) *reinterpret_cast<B *>(dst) = u[i];
     }
   };
   int h = part * a.per;

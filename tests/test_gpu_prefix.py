@@ -217,6 +217,21 @@ def test_two_calls_at_once_on_workspaces_of_their_own():
     assert all(torch.equal(x, y) for pair in got for a, b in zip(pair, want) for x, y in zip(a, b))
 
 
+def test_more_rows_than_one_grid_dimension():
+    """2^24 + 48 rows of two parts, sixteen to a workgroup of the join: 2^20 workgroups and three more."""
+    B, H, Hk, P = 2 ** 20 + 3, 16, 2, 1600
+    config = lambda n: mita.PrefixConfig(n, H, 1, P, 64, H_kv=Hk, N_k=1)
+    g = gen(16)
+    new = lambda *shape: torch.randn((*shape, 64), device="cuda", generator=g, dtype=torch.bfloat16)
+    q, kp, vp, k, v = new(B, H, 1), new(1, Hk, P), new(1, Hk, P), new(B, Hk, 1), new(B, Hk, 1)
+    o, lse = mita.prefix_forward(config(B), q, kp, vp, k, v, o=torch.full_like(q, float("nan")))
+    assert bool(torch.isfinite(o).all()) and bool(torch.isfinite(lse).all())
+    for at in (0, 2 ** 19, B - 16, B - 8):
+        i = slice(at, at + 8)
+        R = expected(config(8), (q[i], kp, vp, k[i], v[i]), None, None, None)
+        assert max(worst(o[i], R.o, R.eo), worst(lse[i], R.lse, R.elz)) <= 1.0
+
+
 def test_without_log_sum_exps():
     cfg = mita.PrefixConfig(3, 2, 1, 900, 64, N_k=10)
     t = make(cfg, "bhnd", 14)

@@ -101,6 +101,10 @@ def check(cfg, layout="bhnd", pos="count", seed=1):
         q2, k2 = (torch.empty_strided(t.shape, t.stride(), dtype=dt, device="cuda").copy_(t) for t in (q, k))
         fn(cfg, q2, k2, p, q2, k2)
         assert torch.equal(q2, qo) and torch.equal(k2, ko)
+        q2 = torch.empty_strided(q.shape, q.stride(), dtype=dt, device="cuda").copy_(q)
+        k2 = torch.full_like(k, float("nan"))
+        fn(cfg, q2, k, p, q2, k2)  # one of them in place
+        assert torch.equal(q2, qo) and torch.equal(k2, ko)
         only, none = fn(cfg, q, pos=p)
         assert torch.equal(only, qo) and none is None
     log(f"[rope] {cfg} {layout} {pos}: " + " ".join(f"{n} {v:.3f}" for n, v in e.items()))
@@ -218,6 +222,23 @@ def test_only_the_tensors_are_written():
     keep = torch.ones(x.shape, dtype=torch.bool)
     keep[:, 1:25, :2, :, :32] = False
     assert torch.equal(x.cpu()[keep], before.cpu()[keep])
+
+
+def test_values_that_are_not_finite():
+    # a NaN or an infinity stays in its pair; what does not turn is copied bit for bit
+    cfg = mita.RopeConfig(2, 2, 30, 64, rot=32)
+    g = gen(10)
+    q = torch.randn((2, 2, 30, 64), device="cuda", generator=g).bfloat16()
+    ok, _ = mita.rope_forward(cfg, q)
+    bad = q.clone()
+    bad[0, 1, 7, 3], bad[1, 0, 9, 20] = float("nan"), float("inf")
+    bad.view(torch.int16)[..., 40:] = torch.randint(-2 ** 15, 2 ** 15, (2, 2, 30, 24), device="cuda", generator=g).short()
+    y, _ = mita.rope_forward(cfg, bad)
+    keep = torch.ones(q.shape, dtype=torch.bool, device="cuda")
+    keep[0, 1, 7, [3, 19]] = keep[1, 0, 9, [4, 20]] = False
+    keep[..., 40:] = False
+    assert torch.equal(y[keep], ok[keep]) and not torch.isfinite(y[0, 1, 7, [3, 19]]).any()
+    assert torch.equal(y[..., 32:].view(torch.int16), bad[..., 32:].view(torch.int16))
 
 
 def test_offsets_past_32_bits():
