@@ -541,7 +541,8 @@ int mita_rms_backward(const mita_rms_cfg_t *cfg, const void *h, const void *w, c
  * For contexts longer than the trained one:
  *   MITA_ROPE_LINEAR  f_i / factor;
  *   MITA_ROPE_BASE    base factor^(rot / (rot - 2)) in base's place, which leaves
- *                     the first pair and divides the last one's f by factor (rot > 2);
+ *                     the first pair and divides the last one's f by factor
+ *                     (a single pair stays as it is);
  *   MITA_ROPE_PARTS   by the turns t a pair makes over `trained` positions: f_i
  *                     where t >= fast, f_i / factor where t <= slow, between them
  *                     c f_i + (1 - c) f_i / factor with c = (t - slow) / (fast - slow).

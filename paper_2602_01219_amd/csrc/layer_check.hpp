@@ -483,7 +483,6 @@ inline int check_rope(const mita_rope_cfg_t *c, std::string *err) {
   if (!(c->base > 1.0) || std::isinf(c->base)) return fail(MITA_ERR_INVALID_ARG, "base must be finite and > 1");
   if (c->scaling != MITA_ROPE_NONE && (!(c->factor >= 1.0) || std::isinf(c->factor)))
     return fail(MITA_ERR_INVALID_ARG, "factor must be finite and >= 1");
-  if (c->scaling == MITA_ROPE_BASE && c->rot < 4) return fail(MITA_ERR_INVALID_ARG, "MITA_ROPE_BASE needs rot >= 4");
   if (c->scaling == MITA_ROPE_PARTS) {
     if (c->trained < 1) return fail(MITA_ERR_INVALID_ARG, "trained must be >= 1");
     if (!(c->slow >= 0.0) || !(c->fast > c->slow) || std::isinf(c->fast))
@@ -510,8 +509,9 @@ inline int check_rope(const mita_rope_cfg_t *c, std::string *err) {
 }
 // Turns per position of each pair, rot / 2 of them.
 inline void rope_turns(const mita_rope_cfg_t &c, double *f) {
-  const double two_pi = 6.283185307179586476925286766559, base =
-      c.scaling == MITA_ROPE_BASE ? c.base * std::pow(c.factor, (double)c.rot / (c.rot - 2)) : c.base;
+  const double two_pi = 6.283185307179586476925286766559;
+  // (one pair alone has f = 1 for any base)
+  const double base = c.scaling == MITA_ROPE_BASE && c.rot > 2 ? c.base * std::pow(c.factor, (double)c.rot / (c.rot - 2)) : c.base;
   for (int i = 0; i < c.rot / 2; ++i) {
     double t = std::pow(base, -2.0 * i / c.rot) / two_pi;
     if (c.scaling == MITA_ROPE_LINEAR) t /= c.factor;

@@ -25,7 +25,7 @@ F64 = torch.float64
 def rates(cfg):
     """Radians per position of each pair."""
     rot, base = cfg.rot or cfg.d, cfg.base
-    if cfg.scaling == "base":
+    if cfg.scaling == "base" and rot > 2:
         base *= cfg.factor ** (rot / (rot - 2))
     out = []
     for i in range(rot // 2):
@@ -139,7 +139,7 @@ def test_sizes(shape):
 @pytest.mark.parametrize("scaling", ["linear", "base", "parts"])
 def test_long_contexts(scaling, dtype):
     more = dict(trained=4096, slow=1.0, fast=32.0, scale=1.3) if scaling == "parts" else {}
-    for d, rot in ((64, 0), (128, 64)):
+    for d, rot in ((64, 0), (128, 64), (64, 2), (64, 4)):
         check(mita.RopeConfig(1, 2, 700, d, rot=rot, dtype=dtype, scaling=scaling, factor=8.0, first=100000, **more))
 
 
@@ -222,6 +222,20 @@ def test_only_the_tensors_are_written():
     keep = torch.ones(x.shape, dtype=torch.bool)
     keep[:, 1:25, :2, :, :32] = False
     assert torch.equal(x.cpu()[keep], before.cpu()[keep])
+
+
+def test_grouped_heads_in_place_in_a_fused_projection():
+    # 6 query heads, 2 key heads and 2 value heads of a token side by side
+    g = gen(11)
+    x = torch.randn((2, 30, 10, 64), device="cuda", generator=g).bfloat16()
+    before = x.clone()
+    q, k = x[:, :, :6].transpose(1, 2), x[:, :, 6:8].transpose(1, 2)
+    cfg = mita.RopeConfig(2, 6, 30, 64, H_kv=2)
+    want = mita.rope_forward(cfg, q, k)
+    mita.rope_forward(cfg, q, k, qo=q, ko=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(x[:, :, 8:], before[:, :, 8:])
+    with pytest.raises(mita.MitaError):  # the keys' output one head into the queries
+        mita.rope_forward(cfg, q, k, qo=q, ko=x[:, :, 5:7].transpose(1, 2))
 
 
 def test_values_that_are_not_finite():

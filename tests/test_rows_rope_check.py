@@ -62,7 +62,7 @@ def test_rope_configurations():
     assert ok(base=1.0) == BAD and ok(base=float("nan")) == BAD and ok(base=float("inf")) == BAD
     assert ok(scale=-1.0) == BAD and ok(scale=float("nan")) == BAD
     assert ok(scaling="linear", factor=0.5) == BAD and ok(scaling="linear", factor=float("inf")) == BAD
-    assert ok(scaling="base", rot=2, factor=2.0) == BAD
+    assert ok(scaling="base", rot=2, factor=2.0) == mita.MITA_OK
     assert ok(scaling="parts", factor=2.0) == BAD and ok(scaling="parts", factor=2.0, trained=10) == mita.MITA_OK
     assert ok(scaling="parts", trained=10, slow=2.0, fast=2.0) == BAD and ok(scaling="parts", trained=10, slow=-1.0) == BAD
     for kw in (dict(scaling="ntk"), dict(dtype="f16"), dict(first=2 ** 31 + 1), dict(N=2 ** 32), dict(scale=1e-60),
