@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 import operator
 import os
@@ -717,18 +718,18 @@ def _lengths(t, name, B, device):
 class _Plan:
     """What a call needs besides addresses, for one configuration and the shapes,
     strides, types and devices of its tensors (never their addresses)."""
-    __slots__ = ("cfg", "ref", "need", "device", "index", "outs")
+    __slots__ = ("cfg", "ref", "need", "device", "index", "make")
 
     def __init__(self, struct, need, device, outs):
         self.cfg, self.ref, self.need, self.device, self.index = struct, ctypes.byref(struct), need, device, device.index
-        self.outs = outs  # per output: (shape, strides, dtype)
+        # makes each output: outs holds (shape, strides, dtype), or None where there is none
+        self.make = [o and functools.partial(torch.empty_strided, o[0], o[1], dtype=o[2], device=device) for o in outs]
 
     def out(self, t, i):
-        return self.new(i) if t is None else t
+        return self.make[i]() if t is None else t
 
     def new(self, i):
-        shape, strides, dtype = self.outs[i]
-        return torch.empty_strided(shape, strides, dtype=dtype, device=self.device)
+        return self.make[i]()
 
 
 def _like(t):
@@ -800,7 +801,7 @@ def _ws_for(plan, ws):
 def _call(plan, fn, args, stream):
     """fn(cfg, *args, stream) with the tensors' device current."""
     raw = torch._C._cuda_getCurrentRawStream(plan.index) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == plan.index:
+    if torch._C._cuda_getDevice() == plan.index:
         st = fn(plan.ref, *args, raw)
     else:
         with torch.cuda.device(plan.index):
