@@ -59,8 +59,13 @@ template <typename T, int D> struct RowTile {
 __device__ __forceinline__ uint32_t lds_at(char *p) {  // address of the workgroup's LDS
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t *)p);
 }
+// ONCE: the launch reads these bytes once, so caches give them up first.
+template <bool ONCE = false>
 __device__ __forceinline__ void copy16_unwaited(const char *base, uint32_t off, uint32_t at) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(at) : "memory");
+  if constexpr (ONCE)
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "{m0}"(at) : "memory");
+  else
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(at) : "memory");
 }
 
 __device__ __forceinline__ void copy16_unwaited(const char *src, uint32_t at) {  // any 64-bit address per lane
@@ -94,7 +99,7 @@ __device__ __forceinline__ void wait_lds() {
 // copy `ins` fills slot l % CPR of row ins * RPI + l / CPR. swz is linear over the
 // bits of the row, and a wave's copies j differ in bits of their own, so copy j's
 // chunk is that of its first XOR swz(j RPI).
-template <typename T, int D, int NW> struct TileCopy {
+template <typename T, int D, int NW, bool ONCE = false> struct TileCopy {
   using RT = RowTile<T, D>;
   static constexpr int PW = RT::TR / RT::RPI / NW;  // copies per wave
   static_assert(PW >= 1 && RT::TR % (RT::RPI * NW) == 0, "whole copies per wave");
@@ -122,11 +127,11 @@ template <typename T, int D, int NW> struct TileCopy {
     if (nrows >= RT::TR) {
 #pragma unroll
       for (int j = 0; j < PW; ++j)
-        copy16_unwaited(src + (uint64_t)(j * RT::RPI) * stride, off0 + chunk(j), tile + (w * PW + j) * 1024);
+        copy16_unwaited<ONCE>(src + (uint64_t)(j * RT::RPI) * stride, off0 + chunk(j), tile + (w * PW + j) * 1024);
     } else {
 #pragma unroll
       for (int j = 0; j < PW; ++j)
-        copy16_unwaited(src, min(row(j), (uint32_t)(nrows - 1)) * stride + chunk(j), tile + (w * PW + j) * 1024);
+        copy16_unwaited<ONCE>(src, min(row(j), (uint32_t)(nrows - 1)) * stride + chunk(j), tile + (w * PW + j) * 1024);
     }
   }
 };

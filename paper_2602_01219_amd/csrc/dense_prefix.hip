@@ -186,7 +186,7 @@ template <typename T, int D> __device__ __forceinline__ const char *key_base(con
 
 // 128 rows, 32 per wave, which share tiles of 64 (fp32: 32) keys: a wave forms the scores
 // of the next tile while it weighs the present one, as dense_fwd_kernel does.
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __device__ __forceinline__ void prefix_tile(const PrefixArgs &a, const PrefixItem &it, char *ldsK, char *ldsV,
                                             PrefixBounds *join) {
   using RT = RowTile<T, D>;
@@ -217,7 +217,7 @@ __device__ __forceinline__ void prefix_tile(const PrefixArgs &a, const PrefixIte
 
   TileAddr<T, D> ad;
   ad.init();
-  TileCopy<T, D, 4> copy;
+  TileCopy<T, D, 4, ONCE> copy;
   copy.init();
   const char *kpb = key_base<T, D>(a.kp, it.bp, it.hk), *vpb = key_base<T, D>(a.vp, it.bp, it.hk);
   const char *kb = key_base<T, D>(a.k, it.b0, it.hk), *vb = key_base<T, D>(a.v, it.b0, it.hk);
@@ -282,7 +282,7 @@ __device__ __forceinline__ void prefix_tile(const PrefixArgs &a, const PrefixIte
 
 // 32 rows whose keys four waves take in turn, 32 at a time, each with tiles of its own in
 // LDS and no barrier, as dense_few_kernel does.
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __device__ __forceinline__ void prefix_few(const PrefixArgs &a, const PrefixItem &it, char *ldsK, char *ldsV,
                                            float (*join_m)[32], float (*join_l)[32]) {
   using FT = FewTile<T, D>;
@@ -303,13 +303,13 @@ __device__ __forceinline__ void prefix_few(const PrefixArgs &a, const PrefixItem
     const bool o = tl.own(t);
     const int k0 = tl.key(t);
     const uint32_t stride = scalar(o ? a.k.n : a.kp.n);
-    few_copy<T, D>(atK, scalar((o ? kb : kpb) + (int64_t)k0 * stride), 0, stride, (o ? tl.kl : tl.pl) - k0);
+    few_copy<T, D, ONCE>(atK, scalar((o ? kb : kpb) + (int64_t)k0 * stride), 0, stride, (o ? tl.kl : tl.pl) - k0);
   };
   auto copy_v = [&](int t) {
     const bool o = tl.own(t);
     const int k0 = tl.key(t);
     const uint32_t stride = scalar(o ? a.v.n : a.vp.n);
-    few_copy<T, D>(atV, scalar((o ? vb : vpb) + (int64_t)k0 * stride), 0, stride, (o ? tl.kl : tl.pl) - k0);
+    few_copy<T, D, ONCE>(atV, scalar((o ? vb : vpb) + (int64_t)k0 * stride), 0, stride, (o ? tl.kl : tl.pl) - k0);
   };
   TileAddr<T, D> ad;
   ad.init();
@@ -373,7 +373,7 @@ __device__ __forceinline__ void prefix_few(const PrefixArgs &a, const PrefixItem
 // prefixes' rows by tiles of 128 or 32 and each sequence's by 32.
 enum { WAY_TILE, WAY_FEW, WAY_SHARED_TILE, WAY_SHARED_FEW };
 
-template <typename T, int D, int WAY>
+template <typename T, int D, int WAY, bool ONCE>
 __global__ void __launch_bounds__(256, WAY == WAY_FEW || WAY == WAY_SHARED_FEW ? (sizeof(T) * D == 128 ? 4 : sizeof(T) * D == 256 ? 2 : 1)
                                                                               : sizeof(T) * D <= 256 ? 2 : 1)
     prefix_kernel(PrefixArgs a) {
@@ -434,9 +434,9 @@ __global__ void __launch_bounds__(256, WAY == WAY_FEW || WAY == WAY_SHARED_FEW ?
     it.slot = a.splits + it.sp;
   }
   if (tile && (!shared || (int)blockIdx.x < a.blocks))
-    prefix_tile<T, D>(a, it, ldsK, ldsV, join.bounds);
+    prefix_tile<T, D, ONCE>(a, it, ldsK, ldsV, join.bounds);
   else if (WAY != WAY_TILE)
-    prefix_few<T, D>(a, it, ldsK, ldsV, join.of[0], join.of[1]);
+    prefix_few<T, D, ONCE>(a, it, ldsK, ldsV, join.of[0], join.of[1]);
 }
 
 // Joins a row's parts by their log-sum-exps. ROWS = 1: a workgroup per row, whose groups
@@ -509,14 +509,20 @@ template <typename T, int D, int ROWS> __global__ void __launch_bounds__(256) pr
 
 template <typename T, int D> hipError_t forward_t(const PrefixArgs &a, const PrefixPlan &p, hipStream_t st) {
   const dim3 grid((unsigned)(p.blocks + p.oblocks));
-  if (p.shared && p.few)
-    prefix_kernel<T, D, WAY_SHARED_FEW><<<grid, 256, 0, st>>>(a);
+  if (p.shared && p.few && p.once)
+    prefix_kernel<T, D, WAY_SHARED_FEW, true><<<grid, 256, 0, st>>>(a);
+  else if (p.shared && p.few)
+    prefix_kernel<T, D, WAY_SHARED_FEW, false><<<grid, 256, 0, st>>>(a);
+  else if (p.shared && p.once)
+    prefix_kernel<T, D, WAY_SHARED_TILE, true><<<grid, 256, 0, st>>>(a);
   else if (p.shared)
-    prefix_kernel<T, D, WAY_SHARED_TILE><<<grid, 256, 0, st>>>(a);
+    prefix_kernel<T, D, WAY_SHARED_TILE, false><<<grid, 256, 0, st>>>(a);
+  else if (p.few && p.once)
+    prefix_kernel<T, D, WAY_FEW, true><<<grid, 256, 0, st>>>(a);
   else if (p.few)
-    prefix_kernel<T, D, WAY_FEW><<<grid, 256, 0, st>>>(a);
+    prefix_kernel<T, D, WAY_FEW, false><<<grid, 256, 0, st>>>(a);
   else
-    prefix_kernel<T, D, WAY_TILE><<<grid, 256, 0, st>>>(a);
+    prefix_kernel<T, D, WAY_TILE, false><<<grid, 256, 0, st>>>(a);
   const hipError_t e = launched("prefix_kernel", st);
   if (e != hipSuccess || p.slots == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.rows;

@@ -88,7 +88,7 @@ template <typename T, int D> struct FewTile {
 };
 
 // The wave's next tile: rows past the last repeat it.
-template <typename T, int D>
+template <typename T, int D, bool ONCE = false>
 __device__ __forceinline__ void few_copy(uint32_t tile, const char *base, int first, uint32_t stride, int nrows) {
   using RT = RowTile<T, D>;
   const int lane = threadIdx.x & 63;
@@ -96,8 +96,8 @@ __device__ __forceinline__ void few_copy(uint32_t tile, const char *base, int fi
 #pragma unroll
   for (int j = 0; j < FewTile<T, D>::NI; ++j) {
     const int r = j * RT::RPI + lane / RT::CPR;
-    copy16_unwaited(src, (uint32_t)min(r, nrows - 1) * stride + (uint32_t)(((lane % RT::CPR) ^ RT::swz(r)) << 4),
-                    tile + j * 1024);
+    copy16_unwaited<ONCE>(src, (uint32_t)min(r, nrows - 1) * stride + (uint32_t)(((lane % RT::CPR) ^ RT::swz(r)) << 4),
+                          tile + j * 1024);
   }
 }
 

@@ -607,6 +607,7 @@ struct PrefixPlan {
   int otiles, osplits;  // shared: of a sequence's own part (0 without own keys)
   int64_t blocks, oblocks;  // workgroups
   int slots;          // parts of a row's result; 1: none is kept
+  bool once;          // the keys are read once, or by a few row tiles at a time, and are more than caches keep
 };
 // Key splits of `tiles` row tiles of DENSE_TQ rows that go through `keys` keys each. A CU
 // with n of their parts takes, per key, `alone` ns for one and `pair` for each of more,
@@ -627,9 +628,16 @@ inline int prefix_splits(const mita_prefix_cfg_t &c, int64_t tiles, int64_t keys
   }
   return best;
 }
+// Bytes of keys and values from which on caches are told to give them up first (the
+// last-level one holds 256 MB). With it and without, us: 32768 prefix keys and 32 x 1024 own
+// ones of 8 heads, d = 128 (268 MB) 55 and 62; 4 x 5000 and 48 x 300 of 12 heads, d = 64 (106
+// MB) 22.8 and 23.7; four row tiles of 32768 keys (265 MB) 108 and 112; 50 MB that the next
+// call reads again 33 and 32.
+constexpr int64_t PREFIX_ONCE = (int64_t)1 << 26;
 inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
   PrefixPlan p{};
   const int64_t rows = dense_rows(c), S = c.B / c.Bp, keys = (int64_t)c.P + c.N_k;
+  const int64_t bytes = 2 * c.H_kv * ((int64_t)c.Bp * c.P + (int64_t)c.B * c.N_k) * c.d * (int64_t)elem_bytes(c);
   // Together and apart, us, bf16, d = 128, 8 key heads: 1 row of 64 sequences, 1000 prefix
   // keys 21 and 21, 4000 24 and 51; 4 rows of 16, 500 keys 12 and 13, 2000 15 and 18, 8000 19
   // and 35; 8 rows of 16, 1000 keys 16 and 15, 2000 17 and 18; 16 rows of 16, 2000 keys 20
@@ -653,6 +661,7 @@ inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
       p.oblocks = own * p.osplits;
     }
     p.slots = p.splits + p.osplits;
+    p.once = p.tiles <= 4 && bytes >= PREFIX_ONCE;
     return p;
   }
   // Rows by 32 and by 128, us, bf16, d = 128: 96 tiles of 128 rows and 1000 keys 17 and 25,
@@ -664,6 +673,7 @@ inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
     p.tiles = (int)((rows + DENSE_FEW - 1) / DENSE_FEW);
     const int64_t blocks = slices(c) * p.tiles, least = rows <= DENSE_FEW ? 256 : 1024;
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({2 * CUS / blocks, keys / least, PREFIX_MAX_SPLITS}));
+    p.once = S == 1 && p.tiles == 1 && bytes >= PREFIX_ONCE;
   } else {
     p.splits = prefix_splits(c, slices(c) * p.tiles, keys);
   }

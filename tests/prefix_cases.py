@@ -18,6 +18,10 @@ CASES = [
     # many prefixes, whose keys are not split
     (24, 12, 12, 12, 1, 1030, 9, "bnhd", -1, 0, None, [1030 - 90 * i for i in range(12)], None),
     (297, 9, 16, 16, 1, 1030, 3, "bhnd", -1, 0, None, [1030 - 100 * i for i in range(9)], None),
+    # keys and values of 64 MB and more: with sharing (few rows and many), and without
+    (12, 1, 8, 8, 1, 40000, 2000, "bnhd", -1, 0, None, [39999], [2000 - 150 * i for i in range(12)]),
+    (140, 2, 16, 8, 1, 9000, 400, "bhnd", -1, 0, None, [9000, 8191], [400 - 2 * i for i in range(140)]),
+    (3, 3, 8, 8, 1, 30000, 700, "bhnd", -1, 0, None, [30000, 1, 0], [700, 0, 65]),
     # windows that hide some, or all, of a prefix, or reach over its end
     (8, 2, 4, 2, 2, 500, 200, "bnhd", 230, 0, None, [500, 400], [200, 10, 0, 199, 100, 3, 2, 1]),
     (8, 2, 4, 2, 2, 1500, 200, "bnhd", 230, 0, None, [1500, 400], [200, 10, 0, 199, 100, 3, 2, 1]),

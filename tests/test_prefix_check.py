@@ -80,7 +80,7 @@ int main() {
     const size_t parts = (size_t)slices(c) * dense_rows(c) * p.slots;
     if (p.slots > 1 && (L.part_lse < parts * 64 * 4 || L.total < L.part_lse + parts * 4)) return 5;
     if (p.blocks + p.oblocks >= (1 << 24)) return 6;
-    printf("%d %d %d %d\\n", p.shared, p.few, p.splits > 1, p.osplits > 1);
+    printf("%d %d %d %d %d\\n", p.shared, p.few, p.splits > 1, p.osplits > 1, p.once);
   }
   return 0;
 }
@@ -101,9 +101,10 @@ def plans(tmp_path, calls):
 def test_the_gpu_tests_meet_every_way(tmp_path):
     got = plans(tmp_path, [c[:7] + c[8:10] for c in CASES])
     assert len(got) == len(CASES)
-    ways = {(shared, few, split) for shared, few, split, _ in got}
+    ways = {(shared, few, split) for shared, few, split, _, _ in got}
     assert ways == {(s, f, p) for s in (0, 1) for f in (0, 1) for p in (0, 1)}
-    assert {own for shared, _, _, own in got if shared} == {0, 1}
+    assert {own for shared, _, _, own, _ in got if shared} == {0, 1}
+    assert {(shared, few) for shared, few, _, _, once in got if once} == {(1, 1), (1, 0), (0, 1)}
 
 
 def test_plans_hold_over_the_range(tmp_path):
