@@ -551,7 +551,7 @@ int mita_rms_backward(const mita_rms_cfg_t *cfg, const void *h, const void *w, c
  */
 typedef struct {
   int32_t B, H, H_kv, N;   /* H_kv: key heads (no relation to H is needed); H, H_kv at most 4096 */
-  int32_t d, rot;          /* head dim in [2, MITA_ROPE_MAX_D], B N d at most 2^32 - 512; rot even in [2, d] */
+  int32_t d, rot;          /* head dim in [2, MITA_ROPE_MAX_D], B N d at most 2^31 - 512; rot even in [2, d] */
   int32_t dtype;           /* MITA_F32 or MITA_BF16 */
   int32_t interleaved;
   int32_t scaling;         /* MITA_ROPE_* */

@@ -475,9 +475,10 @@ inline int check_rope(const mita_rope_cfg_t *c, std::string *err) {
   if (c->d > MITA_ROPE_MAX_D) return fail(MITA_ERR_UNSUPPORTED, "d must not exceed MITA_ROPE_MAX_D");
   if (c->rot < 2 || c->rot > c->d || c->rot % 2 != 0) return fail(MITA_ERR_INVALID_ARG, "rot must be even and in [2, d]");
   if (c->H > 4096 || c->H_kv > 4096) return fail(MITA_ERR_UNSUPPORTED, "H and H_kv must not exceed 4096");
-  // a thread for each piece of a token, of which a launch has less than 2^32
-  if ((int64_t)c->B * c->N > (1 << 30) || (int64_t)c->B * c->N * c->d > ((int64_t)1 << 32) - 512)
-    return fail(MITA_ERR_UNSUPPORTED, "B * N * d must not exceed 2^32 - 512");
+  // a thread for each piece of a token, of the queries and of the keys, of which a launch
+  // has less than 2^32
+  if ((int64_t)c->B * c->N > (1 << 30) || (int64_t)c->B * c->N * c->d > ((int64_t)1 << 31) - 512)
+    return fail(MITA_ERR_UNSUPPORTED, "B * N * d must not exceed 2^31 - 512");
   if (c->scaling < MITA_ROPE_NONE || c->scaling > MITA_ROPE_PARTS)
     return fail(MITA_ERR_UNSUPPORTED, "scaling must be one of MITA_ROPE_*");
   if (!(c->base > 1.0) || std::isinf(c->base)) return fail(MITA_ERR_INVALID_ARG, "base must be finite and > 1");

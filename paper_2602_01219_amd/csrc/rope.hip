@@ -29,8 +29,8 @@ struct RopeArgs {
   int pos_b;
   int B, N, items;   // items: pieces of a token that a thread takes
   int turning;       // of these, the first so many turn
-  int rot, heads, per;  // heads in all, and of a thread
-  int chunks;           // parts of the heads
+  int rot, per[2];      // heads of a thread
+  int chunks, chunks_q; // parts of the heads, and those of the queries, which come first
   int64_t first;
   float scale;
   double f[MITA_ROPE_MAX_D / 2];  // turns per position
@@ -57,45 +57,43 @@ __device__ __forceinline__ void sin_cos_turns(double turns, float &s, float &c) 
   c = (k + 1) & 2 ? -b : b;
 }
 
-template <typename T, int V> __device__ __forceinline__ void get(const char *p, float (&f)[V]) {
-  constexpr int BYTES = V * (int)sizeof(T);
-  if constexpr (BYTES == 16) {
-    unpack16(*reinterpret_cast<const uint4 *>(p), f, (const T *)nullptr);
-  } else if constexpr (BYTES == 8 && sizeof(T) == 4) {
-    const float2 x = *reinterpret_cast<const float2 *>(p);
-    f[0] = x.x;
-    f[1] = x.y;
-  } else if constexpr (BYTES == 4 && sizeof(T) == 2) {
-    const uint32_t x = *reinterpret_cast<const uint32_t *>(p);
-    f[0] = __uint_as_float(x << 16);
-    f[1] = __uint_as_float(x & 0xffff0000u);
-  } else {
-    static_assert(V == 1, "16 bytes, two elements or one");
-    f[0] = to_f32(*reinterpret_cast<const T *>(p));
-  }
-}
-template <typename T, int V> __device__ __forceinline__ void put(char *p, const float (&f)[V]) {
-  constexpr int BYTES = V * (int)sizeof(T);
-  if constexpr (BYTES == 16 && sizeof(T) == 4) {
-    *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  } else if constexpr (BYTES == 16) {
-    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
-                                               pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-  } else if constexpr (BYTES == 8 && sizeof(T) == 4) {
-    *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
-  } else if constexpr (BYTES == 4 && sizeof(T) == 2) {
-    *reinterpret_cast<uint32_t *>(p) = pack_bf16x2(f[0], f[1]);
-  } else {
-    *reinterpret_cast<T *>(p) = from_f32<T>(f[0]);
-  }
-}
-
-// The same elements as they are.
+// V consecutive elements as they are in memory, and in fp32.
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 template <int BYTES> struct Bits;
-template <> struct Bits<16> { using type = uint4; };
-template <> struct Bits<8> { using type = uint2; };
+template <> struct Bits<16> { using type = u32x4; };
+template <> struct Bits<8> { using type = u32x2; };
 template <> struct Bits<4> { using type = uint32_t; };
 template <> struct Bits<2> { using type = uint16_t; };
+template <typename T, int V> using BitsOf = typename Bits<V * (int)sizeof(T)>::type;
+
+template <typename T, int V> __device__ __forceinline__ void unpack(const BitsOf<T, V> &x, float (&f)[V]) {
+  if constexpr (V * sizeof(T) == 16) {
+    unpack16(__builtin_bit_cast(uint4, x), f, (const T *)nullptr);
+  } else if constexpr (V * sizeof(T) == 8) {
+    f[0] = __uint_as_float(x.x);
+    f[1] = __uint_as_float(x.y);
+  } else if constexpr (sizeof(T) == 4) {
+    f[0] = __uint_as_float(x);
+  } else {
+    f[0] = __uint_as_float((uint32_t)x << 16);
+    if constexpr (V == 2) f[1] = __uint_as_float(x & 0xffff0000u);
+  }
+}
+template <typename T, int V> __device__ __forceinline__ BitsOf<T, V> pack(const float (&f)[V]) {
+  if constexpr (V * sizeof(T) == 16 && sizeof(T) == 4)
+    return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+  else if constexpr (V * sizeof(T) == 16)
+    return u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+  else if constexpr (V * sizeof(T) == 8)
+    return u32x2{__float_as_uint(f[0]), __float_as_uint(f[1])};
+  else if constexpr (sizeof(T) == 4)
+    return __float_as_uint(f[0]);
+  else if constexpr (V == 2)
+    return pack_bf16x2(f[0], f[1]);
+  else
+    return f32_to_bf16(f[0]);
+}
 
 __device__ __forceinline__ void turn(float &u, float &v, float sn, float cs) {
   const float y = u, z = v;
@@ -119,9 +117,18 @@ template <typename T, int V, bool IL> __global__ void __launch_bounds__(256) rop
   const bool turns = item < a.turning;
   // the first element of the item, and where its pairs' other elements are
   const int e0 = turns ? (IL ? 2 * NP * item : V * item) : a.rot + V * (item - a.turning);
+  using B = BitsOf<T, V>;
   constexpr bool second = !IL || V == 1;  // pairs of elements of two pieces
-  const int apart = IL ? (int)sizeof(T) : (a.rot / 2) * (int)sizeof(T);
+  const int apart = !turns ? 0 : IL ? (int)sizeof(T) : (a.rot / 2) * (int)sizeof(T);
+  // a workgroup's heads are all queries' or all keys'
+  const int key = part >= a.chunks_q;
+  const RopeMat &m = a.m[key];
+  int h = (part - key * a.chunks_q) * a.per[key];
+  const int end = min(m.heads, h + a.per[key]);
+  if (!turns && m.same) return;
   float sn[NP], cs[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) sn[i] = 0.f, cs[i] = 1.f;
   if (turns) {
     const double p = a.pos ? (double)a.pos[(int64_t)b * a.pos_b + n] : (double)(a.first + n);
 #pragma unroll
@@ -131,57 +138,41 @@ template <typename T, int V, bool IL> __global__ void __launch_bounds__(256) rop
       cs[i] *= fabsf(a.scale);
     }
   }
-  auto places = [&](int i, const char *&src, char *&dst) {  // of head i; whether its elements stay as they are
-    const bool key = i >= a.m[0].heads;
-    const RopeMat &m = a.m[key];
-    const int h = key ? i - a.m[0].heads : i;
-    src = m.in + b * m.ib + h * m.ih + n * m.in_n + e0 * (int)sizeof(T);
-    dst = m.out + b * m.ob + h * m.oh + n * m.on + e0 * (int)sizeof(T);
-    return m.same;
-  };
-  // U heads, all read before the first is written
-  auto heads = [&](int h, auto count) {
+  const char *src = m.in + b * m.ib + n * m.in_n + e0 * (int)sizeof(T) + h * m.ih;
+  char *dst = m.out + b * m.ob + n * m.on + e0 * (int)sizeof(T) + h * m.oh;
+  const int64_t ih = m.ih, oh = m.oh;
+  // U heads, all read before the first is written. Lanes whose elements do not turn do the
+  // same with theirs, and write them as they were: with a branch of their own their loads
+  // would wait for the others' (4 x 4096 tokens of 32 heads, 32 of 128 elements: 58 us).
+  auto heads = [&](auto count) {
     constexpr int U = decltype(count)::value;
-    const char *src;
-    char *dst;
-    if (turns) {
-      float u[U][V], v[U][V];
+    B u[U], v[U];
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        places(h + i, src, dst);
-        get<T, V>(src, u[i]);
-        if constexpr (second) get<T, V>(src + apart, v[i]);
+    for (int i = 0; i < U; ++i) {
+      u[i] = *reinterpret_cast<const B *>(src + i * ih);
+      if constexpr (second) v[i] = *reinterpret_cast<const B *>(src + i * ih + apart);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      float x[V], y[V];
+      unpack<T, V>(u[i], x);
+      if constexpr (second) unpack<T, V>(v[i], y);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        if constexpr (second)
+          turn(x[j], y[j], sn[j], cs[j]);
+        else
+          turn(x[2 * j], x[2 * j + 1], sn[j], cs[j]);
       }
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        places(h + i, src, dst);
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-          if constexpr (second)
-            turn(u[i][j], v[i][j], sn[j], cs[j]);
-          else
-            turn(u[i][2 * j], u[i][2 * j + 1], sn[j], cs[j]);
-        }
-        put<T, V>(dst, u[i]);
-        if constexpr (second) put<T, V>(dst + apart, v[i]);
+      *reinterpret_cast<B *>(dst + i * oh) = turns ? pack<T, V>(x) : u[i];
+      if constexpr (second) {
+        if (turns) *reinterpret_cast<B *>(dst + i * oh + apart) = pack<T, V>(y);
       }
-    } else {
-      using B = typename Bits<V * (int)sizeof(T)>::type;
-      B u[U];
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        places(h + i, src, dst);
-        u[i] = *reinterpret_cast<const B *>(src);
-      }
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (!places(h + i, src, dst)) *reinterpret_cast<B *>(dst) = u[i];
     }
   };
-  int h = part * a.per;
-  const int end = min(a.heads, h + a.per);
-  for (; h + 4 <= end; h += 4) heads(h, std::integral_constant<int, 4>{});
-  for (; h < end; ++h) heads(h, std::integral_constant<int, 1>{});
+  for (; h + 4 <= end; h += 4, src += 4 * ih, dst += 4 * oh) heads(std::integral_constant<int, 4>{});
+  for (; h + 2 <= end; h += 2, src += 2 * ih, dst += 2 * oh) heads(std::integral_constant<int, 2>{});
+  if (h < end) heads(std::integral_constant<int, 1>{});
 }
 
 // The largest of 16 bytes, two elements and one that every piece of both tensors is
@@ -241,7 +232,7 @@ hipError_t launch_rope(const mita_rope_cfg_t &c, const void *q, const void *k, c
   a.first = c.first;
   const float scale = c.scale != 0.f ? c.scale : 1.f;
   a.scale = back ? -scale : scale;
-  a.heads = c.H + a.m[1].heads;
+  const int heads = c.H + a.m[1].heads;
   rope_turns(c, a.f);
   const int64_t threads = (int64_t)c.B * c.N * a.items, blocks = (threads + 255) / 256;
   // Four heads per thread, whose loads are in flight together, or fewer where that leaves
@@ -249,9 +240,20 @@ hipError_t launch_rope(const mita_rope_cfg_t &c, const void *q, const void *k, c
   // tokens of 40 heads, d = 128: 182 us with one head, 139 with two, 116 with four, 119
   // with eight; 64 x 196 tokens of 12 heads, d = 64: 11.0, 10.0, 10.0, 10.7; one token of
   // 24 sequences, 40 heads: 3.8, 4.1, 4.2, 5.2.
-  const int64_t most = (((int64_t)1 << 32) - 512) / (256 * blocks), least = (a.heads + most - 1) / most;
-  a.per = (int)std::max(least, std::max<int64_t>(1, std::min<int64_t>(4, threads * a.heads / (2 * 4 * 64 * CUS))));
-  a.chunks = (a.heads + a.per - 1) / a.per;
+  int64_t per = std::max<int64_t>(1, std::min<int64_t>(4, threads * heads / (2 * 4 * 64 * CUS)));
+  int chunks[2];
+  for (;; per *= 2) {
+    for (int i = 0; i < 2; ++i) {
+      // (six heads, say, are one part and not two)
+      const int all = a.m[i].heads, n = (int)std::max<int64_t>(1, (all + per / 4) / per);
+      a.per[i] = std::max(1, (all + n - 1) / n);
+      chunks[i] = (all + a.per[i] - 1) / a.per[i];
+    }
+    a.chunks_q = chunks[0];
+    a.chunks = chunks[0] + chunks[1];
+    if (256 * blocks * a.chunks <= ((int64_t)1 << 32) - 512) break;
+    if (per > 8192) return hipErrorInvalidConfiguration;
+  }
   const dim3 grid((unsigned)(blocks * a.chunks));
   const bool il = c.interleaved != 0;
   if (c.dtype == MITA_F32)

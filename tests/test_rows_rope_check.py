@@ -58,7 +58,7 @@ def test_rope_configurations():
     ok = lambda **kw: mita.rope_check(mita.RopeConfig(**{**dict(B=1, H=2, N=3, d=64), **kw}))
     assert ok() == mita.MITA_OK and ok(rot=2) == mita.MITA_OK and ok(d=7, rot=4) == mita.MITA_OK
     assert ok(rot=3) == BAD and ok(rot=66) == BAD and ok(d=7) == BAD and ok(d=1) == BAD and ok(B=0) == BAD
-    assert ok(d=258) == NOT and ok(H=5000) == NOT and ok(B=2 ** 26 + 1, N=1) == NOT and ok(B=2 ** 26 - 8, N=1) == mita.MITA_OK
+    assert ok(d=258) == NOT and ok(H=5000) == NOT and ok(B=2 ** 25, N=1) == NOT and ok(B=2 ** 25 - 8, N=1) == mita.MITA_OK
     assert ok(base=1.0) == BAD and ok(base=float("nan")) == BAD and ok(base=float("inf")) == BAD
     assert ok(scale=-1.0) == BAD and ok(scale=float("nan")) == BAD
     assert ok(scaling="linear", factor=0.5) == BAD and ok(scaling="linear", factor=float("inf")) == BAD
