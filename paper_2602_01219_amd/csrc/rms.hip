@@ -105,10 +105,10 @@ template <int TPR> constexpr int fwd_threads = TPR > NORM_FWD_THREADS ? TPR : NO
 template <int TPR> constexpr int bwd_threads = TPR > NORM_BWD_THREADS ? TPR : NORM_BWD_THREADS;
 
 // One row per thread group and workgroup: what is in flight comes from the other
-// workgroups (two and four rows per group, all loaded first: 84 us and 87 against 84 for
-// 16384 rows of 4096, 9.6 and 12.0 against 8.7 for 2000 of 2048, 27 and 27 against 26 for
-// 300000 of 64).
-template <typename T, int VE, int TPR, int P>
+// workgroups (two and four rows per group, all loaded first, with ordinary reads: 84 us
+// and 87 against 84 for 16384 rows of 4096, 9.6 and 12.0 against 8.7 for 2000 of 2048, 27 and
+// 27 against 26 for 300000 of 64).
+template <typename T, int VE, int TPR, int P, bool ONCE>
 __global__ void __launch_bounds__(fwd_threads<TPR>) rms_fwd_kernel(RmsArgs a) {
   using Sum = RowSum<TPR, fwd_threads<TPR>, 1>;
   using Top = GroupTop<VE, TPR, P, fwd_threads<TPR>>;
@@ -119,8 +119,8 @@ __global__ void __launch_bounds__(fwd_threads<TPR>) rms_fwd_kernel(RmsArgs a) {
   const int t = threadIdx.x % TPR, r = block * Sum::ROWS + threadIdx.x / TPR, rc = min(r, a.rows - 1);
   const bool on = r < a.rows;
   RowRegs<T, VE, TPR, P> x, res;
-  x.load((const T *)a.x + row_at(a, a.sx, rc), a.C, t);
-  if (a.res) res.load((const T *)a.res + row_at(a, a.sres, rc), a.C, t);
+  x.template load<ONCE>((const T *)a.x + row_at(a, a.sx, rc), a.C, t);
+  if (a.res) res.template load<ONCE>((const T *)a.res + row_at(a, a.sres, rc), a.C, t);
   float w[P][VE];
   weights<VE, TPR, P>(w, a.w, a.w16, a.C, t, 1.f);
   float v[P][VE], sum[1] = {0.f};
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(fwd_threads<TPR>) rms_fwd_kernel(RmsArgs a) {
 
 // WG: is dw wanted? A workgroup goes over rows gridDim.x * RPB apart and keeps its
 // columns' sums.
-template <typename T, int VE, int TPR, int P, bool WG>
+template <typename T, int VE, int TPR, int P, bool WG, bool ONCE>
 __global__ void __launch_bounds__(bwd_threads<TPR>) rms_bwd_kernel(RmsArgs a) {
   using Sum = RowSum<TPR, bwd_threads<TPR>, 1>;
   constexpr int RPB = Sum::ROWS;
@@ -208,9 +208,9 @@ __global__ void __launch_bounds__(bwd_threads<TPR>) rms_bwd_kernel(RmsArgs a) {
   for (int r0 = blockIdx.x * RPB; r0 < a.rows; r0 += gridDim.x * RPB) {
     const int r = r0 + sub, rc = min(r, a.rows - 1);
     RowRegs<T, VE, TPR, P> h, y, z;
-    h.load((const T *)a.x + row_at(a, a.sx, rc), a.C, t);
-    y.load((const T *)a.dy + row_at(a, a.sdy, rc), a.C, t);
-    if (a.dh) z.load((const T *)a.dh + row_at(a, a.sdh, rc), a.C, t);
+    h.template load<ONCE>((const T *)a.x + row_at(a, a.sx, rc), a.C, t);
+    y.template load<ONCE>((const T *)a.dy + row_at(a, a.sdy, rc), a.C, t);
+    if (a.dh) z.template load<ONCE>((const T *)a.dh + row_at(a, a.sdh, rc), a.C, t);
     const float rstd = a.rstd_in[row_at(a, a.stat, rc)];
     // lanes past the last row hold its dy, or, with dx in dy's place, what its own
     // lanes have written there by now
@@ -400,16 +400,34 @@ template <typename T> __global__ void __launch_bounds__(512) rms_dw_wide_kernel(
   a.part[(int64_t)blockIdx.y * a.C + i] = dw;
 }
 
+// Inputs of 128 MB and more are read past the caches' order (the last-level one holds 256
+// MB): 16384 rows of 4096 to 8 bits, 268 MB, 77 us, and 86 with ordinary reads; backward of 8192
+// rows of 4096, 201 MB, 49 and 51; 4096 rows of 4096, 67 MB, that are there from the call
+// before, 23 and 20. Pieces of 16 bytes only.
+template <typename T, int VE> bool read_once(const RmsArgs &a, int tensors) {
+  return VE * sizeof(T) == 16 && (int64_t)tensors * a.rows * a.C * (int64_t)sizeof(T) >= (int64_t)1 << 27;
+}
 template <typename T, int VE, int TPR, int P> hipError_t fwd_p(const RmsArgs &a, hipStream_t st) {
   constexpr int N = fwd_threads<TPR>, RPB = N / TPR;
-  rms_fwd_kernel<T, VE, TPR, P><<<rows_grid((a.rows + RPB - 1) / RPB), N, 0, st>>>(a);
+  constexpr bool WHOLE = VE * sizeof(T) == 16;
+  const dim3 grid = rows_grid((a.rows + RPB - 1) / RPB);
+  if (read_once<T, VE>(a, a.res ? 2 : 1))
+    rms_fwd_kernel<T, VE, TPR, P, WHOLE><<<grid, N, 0, st>>>(a);
+  else
+    rms_fwd_kernel<T, VE, TPR, P, false><<<grid, N, 0, st>>>(a);
   return launched("rms_fwd_kernel", st);
 }
 template <typename T, int VE, int TPR, int P> hipError_t bwd_p(const RmsArgs &a, int blocks, hipStream_t st) {
-  if (a.dw)
-    rms_bwd_kernel<T, VE, TPR, P, true><<<dim3((unsigned)blocks), bwd_threads<TPR>, 0, st>>>(a);
+  constexpr bool WHOLE = VE * sizeof(T) == 16;
+  const bool once = read_once<T, VE>(a, a.dh ? 3 : 2);
+  if (a.dw && once)
+    rms_bwd_kernel<T, VE, TPR, P, true, WHOLE><<<dim3((unsigned)blocks), bwd_threads<TPR>, 0, st>>>(a);
+  else if (a.dw)
+    rms_bwd_kernel<T, VE, TPR, P, true, false><<<dim3((unsigned)blocks), bwd_threads<TPR>, 0, st>>>(a);
+  else if (once)
+    rms_bwd_kernel<T, VE, TPR, P, false, WHOLE><<<dim3((unsigned)blocks), bwd_threads<TPR>, 0, st>>>(a);
   else
-    rms_bwd_kernel<T, VE, TPR, P, false><<<dim3((unsigned)blocks), bwd_threads<TPR>, 0, st>>>(a);
+    rms_bwd_kernel<T, VE, TPR, P, false, false><<<dim3((unsigned)blocks), bwd_threads<TPR>, 0, st>>>(a);
   return launched("rms_bwd_kernel", st);
 }
 template <typename T> struct RunFwd {

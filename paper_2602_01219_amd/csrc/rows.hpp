@@ -38,6 +38,11 @@ template <typename T, int VE> struct Piece;
 template <typename T> struct Piece<T, 16 / sizeof(T)> {
   uint4 v;
   __device__ __forceinline__ void load(const T *p) { v = *reinterpret_cast<const uint4 *>(p); }
+  // of tensors that caches do not keep until they are read again
+  __device__ __forceinline__ void load_once(const T *p) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    v = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)));
+  }
   __device__ __forceinline__ void get(float *f) const { unpack16(v, f, (const T *)nullptr); }
 };
 template <> struct Piece<bf16_t, 2> {
@@ -79,9 +84,15 @@ template <typename T, int VE> __device__ __forceinline__ void put(T *p, const fl
 template <typename T, int VE, int TPR, int P> struct RowRegs {
   Piece<T, VE> c[P];
   // pieces past the row repeat its last one (see `get`)
-  __device__ __forceinline__ void load(const T *row, int C, int t) {
+  template <bool ONCE = false> __device__ __forceinline__ void load(const T *row, int C, int t) {
 #pragma unroll
-    for (int j = 0; j < P; ++j) c[j].load(row + min((j * TPR + t) * VE, C - VE));
+    for (int j = 0; j < P; ++j) {
+      const T *p = row + min((j * TPR + t) * VE, C - VE);
+      if constexpr (ONCE)
+        c[j].load_once(p);
+      else
+        c[j].load(p);
+    }
   }
   // piece j in fp32, zero past the row
   __device__ __forceinline__ void get(float (&f)[VE], int j, int C, int t) const {

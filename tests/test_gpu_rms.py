@@ -130,6 +130,14 @@ def test_several_rows_per_thread_group(C, many, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [768, 4096, 8192])
+def test_inputs_of_128_mb_and_more(C, dtype):
+    rows = 2 ** 27 // (C * (2 if dtype == "bf16" else 4)) + 3
+    check((rows,), C, dtype, residual=False, out="e4m3", group=128)
+    check((rows // 2 + 1,), C, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["bnhd", "qkv", "padded"])
 @pytest.mark.parametrize("C", [64, 100, 768])
 def test_strides(C, layout, dtype):

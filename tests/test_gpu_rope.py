@@ -135,6 +135,12 @@ def test_sizes(shape):
     check(mita.RopeConfig(B, H, N, 64, H_kv=Hk, dtype="f32", interleaved=True, first=70000), "bhnd")
 
 
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "inter"])
+@pytest.mark.parametrize("dtype,N,rot", [("bf16", 16390, 0), ("bf16", 16390, 48), ("f32", 8200, 0)])
+def test_inputs_of_128_mb_and_more(dtype, N, rot, interleaved):
+    check(mita.RopeConfig(2, 12, N, 128, H_kv=4, rot=rot, dtype=dtype, interleaved=interleaved), "bnhd")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("scaling", ["linear", "base", "parts"])
 def test_long_contexts(scaling, dtype):
