@@ -11,8 +11,8 @@
 // Prompts are bound by the MFMA and VALU issue, as dense_fwd_kernel: 32 sequences of 512
 // tokens, 16 heads of 4 key heads, behind 8000 keys, d = 128: 1005 us, 1.10 PFLOP/s. Single
 // tokens are bound by the bytes of the keys and by latencies: a token of 32 sequences, 32
-// heads of 8 key heads, behind 32768 keys and up to 1024 of their own, d = 128: 52 us and
-// 5.5 for the join (228 MB: 37 at 6.2 TB/s); of these 3 us pass before the first copy
+// heads of 8 key heads, behind 32768 keys and up to 1024 of their own, d = 128: 46 us and
+// 5 for the join (228 MB: 37 at 6.2 TB/s); of these 3 us pass before the first copy
 // and 2.5 with the writing of the parts, 64 KB of each workgroup.
 #include "dense.hpp"
 #include "dense_softmax.hpp"

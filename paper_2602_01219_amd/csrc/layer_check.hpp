@@ -652,7 +652,8 @@ inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
     const int64_t blocks = prefixes * p.tiles;
     // one workgroup per CU, beside which others take the own keys: a part of 128 rows is
     // 64 KB to write and read again (128 rows of 32768 keys and 8 key heads, each of 32
-    // sequences up to 1024 of its own, d = 128: 61 us with 32 splits, 71 with 16, 72 with 64)
+    // sequences up to 1024 of its own, d = 128, ordinary reads: 61 us with 32 splits, 71 with 16,
+    // 72 with 64)
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({CUS / blocks, c.P / 128, PREFIX_MAX_SPLITS}));
     p.blocks = blocks * p.splits;
     if (c.N_k) {

@@ -401,9 +401,11 @@ template <typename T> __global__ void __launch_bounds__(512) rms_dw_wide_kernel(
 }
 
 // Inputs of 128 MB and more are read past the caches' order (the last-level one holds 256
-// MB): 16384 rows of 4096 to 8 bits, 268 MB, 77 us, and 86 with ordinary reads; backward of 8192
-// rows of 4096, 201 MB, 49 and 51; 4096 rows of 4096, 67 MB, that are there from the call
-// before, 23 and 20. Pieces of 16 bytes only.
+// MB). With it and with ordinary reads, us, inputs and outputs of three calls in turn: 16384 rows
+// of 4096 to 8 bits, 268 MB, 84 and 85 (77 and 86 where the outputs take the place of the
+// call's before); 8192 rows of 4096, 134 MB, 43 and 48, backward, 201 MB, 49 and 56; backward
+// of 65536 rows of 768 70 and 80; but 4096 rows of 4096, 67 MB, that are there from the
+// call before, 23 and 20. Pieces of 16 bytes only.
 template <typename T, int VE> bool read_once(const RmsArgs &a, int tensors) {
   return VE * sizeof(T) == 16 && (int64_t)tensors * a.rows * a.C * (int64_t)sizeof(T) >= (int64_t)1 << 27;
 }

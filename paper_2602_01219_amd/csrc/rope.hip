@@ -5,7 +5,7 @@
 // Bound by HBM: every element is read and written once. A thread turns the same
 // piece (of 16 bytes, or two of them where a head's halves form the pairs) of
 // several heads of one token, so its angles' sines and cosines are formed once for
-// all of them. 32768 tokens of 32 + 8 heads in token order, d = 128, bf16: 116 us, 5.8
+// all of them. 32768 tokens of 32 + 8 heads in token order, d = 128, bf16: 118 us, 5.7
 // TB/s (a plain elementwise product reaches 6.2); 139 with the parts of a token's heads
 // in distant workgroups, which touch the memory's pages in turn.
 #include "cdna4.hpp"
@@ -195,9 +195,11 @@ int rope_vector(const mita_rope_cfg_t &c, const Strided *t, const void *const *p
   return fits(full) ? full : fits(2) ? 2 : 1;
 }
 
-// once: inputs of 128 MB and more are read past the caches' order, as in the RMS norm (4
-// x 8192 tokens of 32 heads, d = 128, heads before tokens, 268 MB: 82 us, and 102 with ordinary
-// reads; tokens before heads 117 either way; 26 MB that are there from the call before 14 and 10).
+// once: inputs of 128 MB and more are read past the caches' order, as in the RMS norm. With it
+// and with ordinary reads, us, inputs and outputs of three calls in turn: 4 x 8192 tokens
+// of 32 heads, d = 128, 268 MB, heads before tokens 99 and 102, tokens before heads 94 and 96;
+// 4 x 4096, 134 MB, 46 and 52; 32768 tokens of 32 + 8 heads 119 and 118; but 26 MB that
+// are there from the call before 14 and 10.
 template <typename T, int V> hipError_t rope_v(const RopeArgs &a, bool il, bool once, dim3 grid, hipStream_t st) {
   constexpr bool WHOLE = V * sizeof(T) == 16;
   if (il && once)
