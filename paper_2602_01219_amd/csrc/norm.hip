@@ -27,13 +27,14 @@ namespace mita {
 
 namespace {
 
-struct NormArgs : RowWalk {
+struct NormTensors {
   const void *x, *dy, *w, *b;
   void *y, *dx, *dw, *db;
   const float *mean_in, *rstd_in;
   float *mean, *rstd, *part;
   RowPlaces sx, sy, sdy, sdx, stat;  // `stat`: of the row's statistics
-  int C;
+};
+struct NormArgs : NormTensors, RowWalk {
   bool w16;  // weights in bf16
   float eps, invC;
 };
@@ -289,7 +290,6 @@ NormArgs norm_args(const mita_norm_cfg_t &c, const Strided *t, int tensors, RowP
   static_cast<RowWalk &>(a) = row_walk(t, tensors, places);
   for (int i = 0; i < tensors; ++i) a.*to[i] = places[i];
   a.stat = places[tensors];
-  a.C = c.C;
   a.w16 = c.wdtype == MITA_BF16;
   a.eps = c.eps;
   a.invC = 1.f / (float)c.C;

@@ -21,7 +21,6 @@ struct RmsArgs : RowWalk {
   const float *rstd_in;
   float *rstd, *scales, *part;
   RowPlaces sx, sres, sh, sy, sdy, sdh, sdx, stat;  // `stat`: of the row's statistics
-  int C;
   int q8;      // y: 0 in the rows' type, 1 in 8 bits with a scale per row, 2 per 128 columns
   int groups;  // scales per row
   bool w16;    // weights in bf16
@@ -473,7 +472,6 @@ template <typename T> hipError_t backward_t(const RmsArgs &a, const NormPlan &p,
 
 RmsArgs rms_args(const mita_rms_cfg_t &c) {
   RmsArgs a{};
-  a.C = c.C;
   a.q8 = c.ytype != MITA_E4M3 ? 0 : c.group ? 2 : 1;
   a.groups = rms_scales(c);
   a.w16 = c.wdtype == MITA_BF16;

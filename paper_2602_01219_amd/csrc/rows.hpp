@@ -17,7 +17,7 @@ struct RowPlaces {
 // Rows are walked in the order of the first tensor in memory, dimensions 0, 1, 2 from
 // the outside in.
 struct RowWalk {
-  int rows, n1, n2;
+  int rows, n1, n2, C;  // C: elements of a row
   uint32_t m1, m2;  // for quotients by n1 and n2
   int h1, h2;
 };
@@ -259,6 +259,7 @@ inline RowWalk row_walk(const Strided *t, int tensors, RowPlaces *places) {
   magic(n[1], a.m1, a.h1);
   magic(n[2], a.m2, a.h2);
   a.rows = (int)(c[0] * c[1] * c[2]);
+  a.C = (int)t[0].len;
   return a;
 }
 
