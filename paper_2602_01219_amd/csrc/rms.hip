@@ -15,12 +15,15 @@ namespace mita {
 
 namespace {
 
-struct RmsArgs : RowWalk {
+struct RmsTensors {
   const void *x, *res, *w, *dy, *dh;
   void *h, *y, *dx, *dw;
   const float *rstd_in;
   float *rstd, *scales, *part;
   RowPlaces sx, sres, sh, sy, sdy, sdh, sdx, stat;  // `stat`: of the row's statistics
+};
+// (the tensors first: 39.1 us for the backward of 32768 rows of 768, 39.5 with the walk first)
+struct RmsArgs : RmsTensors, RowWalk {
   int q8;      // y: 0 in the rows' type, 1 in 8 bits with a scale per row, 2 per 128 columns
   int groups;  // scales per row
   bool w16;    // weights in bf16
