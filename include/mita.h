@@ -506,7 +506,7 @@ size_t mita_rms_workspace_size(const mita_rms_cfg_t *cfg);
  *   rstd : [n0, n1, n2] fp32 contiguous output for the backward pass, or NULL.
  * h, and y in dtype, may each be x or res with the same strides (not both the same
  * one), and must not overlap an input otherwise. Squares are fp32: a row's mean of
- * squares has to stay finite there.
+ * squares has to stay finite there (its sum of squares need not).
  */
 int mita_rms_forward(const mita_rms_cfg_t *cfg, const void *x, const void *res, const void *w, void *h, void *y,
                      float *scales, float *rstd, mita_stream_t stream);
@@ -515,7 +515,7 @@ int mita_rms_forward(const mita_rms_cfg_t *cfg, const void *x, const void *res, 
  * With u = h rstd and g = dy w: dx = dh + rstd (g - u mean(g u)) per row, the
  * gradient of x and of res alike, and dw = sum over rows of dy u. The row sums are
  * added in a fixed order in fp32 (the same bit for bit from call to call) and
- * rounded once.
+ * rounded once. Sums have to stay finite there: C mean|g u| of a row, and a column's.
  *   h : the forward's h (x where there was no residual);  w : the forward's, or NULL;
  *   rstd : the forward's;  dy : gradient of y, in dtype;  dh : gradient of h, or NULL (0);
  *   dx : output or NULL;  dw : [C] output or NULL. dx may be dy or dh with the same

@@ -28,6 +28,10 @@ struct RmsArgs : RmsTensors, RowWalk {
   int groups;  // scales per row
   bool w16;    // weights in bf16
   float eps, invC;
+  // The forward adds squares of v unit, unit = 2^-k with 4^k >= C, and multiplies their sum
+  // by over = 4^k / C, below 4: it stays finite wherever the mean of squares is. Powers of
+  // two change no rounding, but for means below 2^-124, whose sum is denormal.
+  float unit, over;
 };
 
 constexpr float E4M3_MAX = 448.f;
@@ -136,10 +140,13 @@ __global__ void __launch_bounds__(fwd_threads<TPR>) rms_fwd_kernel(RmsArgs a) {
       for (int e = 0; e < VE; ++e) v[j][e] += z[e];
     }
 #pragma unroll
-    for (int e = 0; e < VE; ++e) sum[0] = __builtin_fmaf(v[j][e], v[j][e], sum[0]);
+    for (int e = 0; e < VE; ++e) {
+      const float z = v[j][e] * a.unit;
+      sum[0] = __builtin_fmaf(z, z, sum[0]);
+    }
   }
   row_sum(sum);
-  const float rstd = 1.f / sqrtf(sum[0] * a.invC + a.eps);
+  const float rstd = 1.f / sqrtf(sum[0] * a.over + a.eps);
   if (a.h && on) {
     T *h = (T *)a.h + row_at(a, a.sh, r);
 #pragma unroll
@@ -312,10 +319,10 @@ template <typename T> __global__ void __launch_bounds__(512) rms_fwd_wide_kernel
     };
     float s = 0.f;
     for (int i = threadIdx.x; i < a.C; i += blockDim.x) {
-      const float v = at(i);
-      s = __builtin_fmaf(v, v, s);
+      const float z = at(i) * a.unit;
+      s = __builtin_fmaf(z, z, s);
     }
-    const float rstd = 1.f / sqrtf(block_sum(s, red) * a.invC + a.eps);
+    const float rstd = 1.f / sqrtf(block_sum(s, red) * a.over + a.eps);
     const int64_t stat = row_at(a, a.stat, r);
     if (threadIdx.x == 0 && a.rstd) a.rstd[stat] = rstd;
     if (a.q8 == 0) {
@@ -480,6 +487,10 @@ RmsArgs rms_args(const mita_rms_cfg_t &c) {
   a.w16 = c.wdtype == MITA_BF16;
   a.eps = c.eps;
   a.invC = 1.f / (float)c.C;
+  int k = 0;
+  while (((int64_t)1 << 2 * k) < c.C) ++k;
+  a.unit = 1.f / (float)(1 << k);
+  a.over = (float)((int64_t)1 << 2 * k) * a.invC;
   return a;
 }
 
