@@ -496,8 +496,8 @@ size_t mita_rms_workspace_size(const mita_rms_cfg_t *cfg);
  * h = x + res, rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd w per row, in fp32
  * from the sum before it is rounded to h's type; each output is rounded once.
  * With ytype MITA_E4M3, y is codes and scales: a group's scale is the largest
- * |h rstd w| in it (at least 2^-117) / 448, a code h rstd w / scale rounded to
- * nearest even, and code * scale the value it stands for. Backward, such an output
+ * |h rstd w| in it (at least 2^-117) / 448, a code the fp32 quotient h rstd w / scale
+ * rounded to nearest even, and code * scale the value it stands for. Backward, such an output
  * is differentiated as if it had not been rounded.
  *   res  : or NULL (0);  w : [C], or NULL (1);
  *   h    : output, or NULL (without res it is x's values);

@@ -37,6 +37,40 @@ struct RmsArgs : RmsTensors, RowWalk {
 constexpr float E4M3_MAX = 448.f;
 // The scale of a group whose largest value is `top`: not 0, and its reciprocal finite.
 __device__ __forceinline__ float e4m3_scale(float top) { return fmaxf(top, 0x1p-117f) / E4M3_MAX; }
+// y / scale as fp32 division rounds it, with one reciprocal for several values: a quotient q
+// off by a step or two is brought to one of the two nearest by its residual, and from there
+// to the nearest, as the residual then is exact (Markstein's theorem, 1990; the reciprocal
+// has to be rounded correctly). All of it times the power of two that brings the scale to
+// [1, 2), so that no residual that counts is lost below 2^-149. An infinite scale gives
+// 0, and NaN for infinite y. 16384 rows of 4096 without a residual, bf16: 49 us with a
+// division per value, 42.6 so, 41 with products with the reciprocal, which differ where y /
+// scale is next to the middle of two codes. Pieces of one or two elements are divided.
+struct Quotient {
+  float unit, s, inv;
+  __device__ __forceinline__ explicit Quotient(float scale) {
+    const uint32_t e = __float_as_uint(scale) & 0x7f800000u;
+    unit = __uint_as_float(0x7f000000u - min(e, 0x7e800000u));
+    s = scale * unit;
+    inv = 1.f / s;
+    s = e == 0x7f800000u ? 0.f : s;
+  }
+  __device__ __forceinline__ float operator()(float y) const {
+    y *= unit;
+    float q = y * inv;
+    q = __builtin_fmaf(-__builtin_fmaf(q, s, -y), inv, q);  // (so written, -0 stays -0)
+    return __builtin_fmaf(-__builtin_fmaf(q, s, -y), inv, q);
+  }
+};
+template <int VE> __device__ __forceinline__ void divide(float (&o)[VE], const float (&y)[VE], float scale) {
+  if constexpr (VE > 2) {
+    const Quotient quotient(scale);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) o[e] = quotient(y[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VE; ++e) o[e] = y[e] / scale;
+  }
+}
 // VE codes of values that are at most 448 (but for the last rounding, which the
 // conversion takes back).
 template <int VE> __device__ __forceinline__ void put_e4m3(uint8_t *p, const float *f) {
@@ -183,10 +217,9 @@ __global__ void __launch_bounds__(fwd_threads<TPR>) rms_fwd_kernel(RmsArgs a) {
 #pragma unroll
       for (int j = 0; j < P; ++j) {
         const int i = (j * TPR + t) * VE;
-        const float s = e4m3_scale(top[j]), inv = 1.f / s;
+        const float s = e4m3_scale(top[j]);
         float o[VE];
-#pragma unroll
-        for (int e = 0; e < VE; ++e) o[e] = v[j][e] * inv;
+        divide(o, v[j], s);
         if (i < a.C) {
           put_e4m3<VE>(y + i, o);
           if (a.q8 == 2 ? i % RMS_GROUP == 0 : i == 0) scales[a.q8 == 2 ? i / RMS_GROUP : 0] = s;
@@ -365,10 +398,9 @@ template <typename T> __global__ void __launch_bounds__(512) rms_fwd_wide_kernel
         scale = e4m3_scale(wave_max(fmaxf(fabsf(v[0]), fabsf(v[1]))));
         if ((threadIdx.x & 63) == 0) a.scales[stat * a.groups + c / RMS_GROUP] = scale;
       }
-      const float inv = 1.f / scale;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float o = v[e] * inv;
+        const float o = v[e] / scale;
         if (in[e]) put_e4m3<1>(y + i[e], &o);
       }
     }

@@ -21,7 +21,8 @@ def middles():
 
 
 def weights(C, group, seed):
-    """[C] fp32: in each group one largest value, and multiples of its scale by the middles, moved by up to two steps."""
+    """[C] fp32: in each group a zero, one largest value, and multiples of its scale by the middles, moved by up to two
+    steps."""
     g = torch.Generator().manual_seed(seed)
     width, w = group or C, torch.empty(C)
     m = middles()
@@ -32,7 +33,8 @@ def weights(C, group, seed):
         step = torch.randint(-2, 3, (n,), generator=g, dtype=torch.int32)
         t = (t.view(torch.int32) + step).view(torch.float32)
         t = torch.where(torch.rand(n, generator=g) < 0.5, -t, t)
-        t[torch.randint(n, (1,), generator=g)] = top
+        t[0] = 0.0
+        t[1 + torch.randint(n - 1, (1,), generator=g)] = top
         w[at:at + n] = t
     return w
 
