@@ -606,7 +606,7 @@ typedef struct {
 int mita_prefix_check(const mita_prefix_cfg_t *cfg);
 
 /* Bytes of workspace mita_prefix_forward needs (0 if cfg is invalid). It depends
- * on the sizes, the type and the window, not on the strides. */
+ * on the sizes and the type alone. */
 size_t mita_prefix_workspace_size(const mita_prefix_cfg_t *cfg);
 
 /*
