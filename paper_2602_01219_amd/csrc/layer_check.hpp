@@ -1,6 +1,7 @@
 // layer_check.hpp - host-only validation, launch plans and workspace layouts of
-// the dense attention and the layer norm. Header-only, no HIP dependency: the
-// host test builds it with g++.
+// the dense attention, whole and over shared prefixes, of the layer norm and the RMS
+// norm, and of the rotary positions, with their turns per position. Header-only, no HIP
+// dependency: the host test builds it with g++.
 #pragma once
 #include <algorithm>
 #include <cmath>
@@ -630,12 +631,16 @@ inline int prefix_splits(const mita_prefix_cfg_t &c, int64_t tiles, int64_t keys
   return best;
 }
 // Bytes of keys and values from which on caches are told to give them up first (the
-// last-level one holds 256 MB). With it and without, us: 32768 prefix keys and 32 x 1024 own
-// ones of 8 heads, d = 128 (268 MB) 55 and 62; 4 x 5000 and 48 x 300 of 12 heads, d = 64 (106
-// MB) 22.8 and 23.7; four row tiles of 32768 keys (265 MB) 108 and 112; 50 MB that the next
-// call reads again 33 and 32.
+// last-level one holds 256 MB). With it and without, us, inputs of three calls in turn: 32768
+// prefix keys and 32 x 1024 own ones of 8 heads, d = 128 (268 MB) 57.9 and 65.1; four row
+// tiles of 32768 keys (134 MB) 97.1 and 97.6; 4 x 5000 and 48 x 300 of 12 heads, d = 64 (106 MB)
+// 26.0 and 27.0, and with lengths that leave 84 MB of them 22.8 and 22.7; 8000 and 16 x 256 of
+// 8 heads, d = 128 (50 MB) 22.7 and 20.4.
 constexpr int64_t PREFIX_ONCE = (int64_t)1 << 26;
 inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
+  // (the window is not looked at: parts whose keys it hides find none, write zeros and are
+  // joined. A token of 32 sequences, 32 heads of 8 key heads, behind 32768 keys, d = 128:
+  // 55 us without one, 43 with left = 8192, 30 with 512)
   PrefixPlan p{};
   const int64_t rows = dense_rows(c), S = c.B / c.Bp, keys = (int64_t)c.P + c.N_k;
   const int64_t bytes = 2 * c.H_kv * ((int64_t)c.Bp * c.P + (int64_t)c.B * c.N_k) * c.d * (int64_t)elem_bytes(c);
@@ -643,17 +648,22 @@ inline PrefixPlan prefix_plan(const mita_prefix_cfg_t &c) {
   // keys 21 and 21, 4000 24 and 51; 4 rows of 16, 500 keys 12 and 13, 2000 15 and 18, 8000 19
   // and 35; 8 rows of 16, 1000 keys 16 and 15, 2000 17 and 18; 16 rows of 16, 2000 keys 20
   // and 19, 8000 28 and 35; 32 rows of 16, 8000 keys 39 and 37. Short prefixes have no
-  // splits to join apart (250 keys, 4 rows of 4: 12 and 10).
+  // splits to join apart (250 keys, 4 rows of 4: 12 and 10). From 32 rows on the bound does not
+  // look at how many sequences and keys there are: 40 rows of 16 and of 32 sequences, always
+  // apart, 57 and 97 us behind 8000 keys, 242 and 450 behind 32768, 436 and 820 behind 60000.
   p.shared = S > 1 && rows < DENSE_FEW && c.P >= std::max<int64_t>(1024, 200 * rows);
   if (p.shared) {
     const int64_t prefixes = (int64_t)c.Bp * c.H_kv, all = shared_rows(c);
     p.few = all <= DENSE_FEW;
     p.tiles = (int)((all + (p.few ? DENSE_FEW : DENSE_TQ) - 1) / (p.few ? DENSE_FEW : DENSE_TQ));
     const int64_t blocks = prefixes * p.tiles;
-    // one workgroup per CU, beside which others take the own keys: a part of 128 rows is
-    // 64 KB to write and read again (128 rows of 32768 keys and 8 key heads, each of 32
-    // sequences up to 1024 of its own, d = 128, ordinary reads: 61 us with 32 splits, 71 with 16,
-    // 72 with 64)
+    // one workgroup per CU, beside which others take the own keys (but for fp32 and d = 128,
+    // where the LDS of either fills the CU, and they follow): a part of 128 rows is 64 KB to
+    // write and read again (128 rows of 32768 keys and 8 key heads, each of 32 sequences up
+    // to 1024 of its own, d = 128, ordinary reads: 61 us with 32 splits, 71 with 16, 72 with 64).
+    // 32 rows, one, two and three workgroups per CU, us, 12 of the rows there: 12 heads behind 4
+    // x 5000 and 300 keys, bf16, d = 64 22.9, 24.3 and 25.0, d = 128 39.3, 39.8 and 44.8, fp32
+    // 42, 44 and 48; 16 rows, 8 heads, 32768 and 500 keys, d = 128 36.5, 38.5 and 38.2
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({CUS / blocks, c.P / 128, PREFIX_MAX_SPLITS}));
     p.blocks = blocks * p.splits;
     if (c.N_k) {

@@ -34,6 +34,9 @@ struct NormTensors {
   float *mean, *rstd, *part;
   RowPlaces sx, sy, sdy, sdx, stat;  // `stat`: of the row's statistics
 };
+// (the tensors first, and a row's width beside the number of rows, as in the RMS norm: with
+// others between them the instructions read their arguments at other places, and the
+// backward of 32768 rows of 768 takes 35.0 us instead of 34.4)
 struct NormArgs : NormTensors, RowWalk {
   bool w16;  // weights in bf16
   float eps, invC;

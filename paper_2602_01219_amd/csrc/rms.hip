@@ -22,7 +22,8 @@ struct RmsTensors {
   float *rstd, *scales, *part;
   RowPlaces sx, sres, sh, sy, sdy, sdh, sdx, stat;  // `stat`: of the row's statistics
 };
-// (the tensors first: 39.1 us for the backward of 32768 rows of 768, 39.5 with the walk first)
+// (the tensors first: the walk first gives the same instructions, which read their arguments
+// at other places, and for the backward of 32768 rows of 768 39.8 us instead of 39.5)
 struct RmsArgs : RmsTensors, RowWalk {
   int q8;      // y: 0 in the rows' type, 1 in 8 bits with a scale per row, 2 per 128 columns
   int groups;  // scales per row
@@ -337,7 +338,9 @@ __global__ void __launch_bounds__(512) rms_sum_kernel(RmsArgs a, int parts) {
     ((float *)a.dw)[i] = y;
 }
 
-// Rows too wide for registers: a workgroup per row, which reads it once per pass.
+// Rows too wide for registers: a workgroup per row, which reads it once per pass, element by
+// element: 2000 rows of 32768, bf16, 385 us to 8 bits with a scale per row (three passes; 32
+// at 6.2 TB/s), 470 with a residual to bf16 (85), backward 490.
 // Outputs in an input's place are written in the last one, each element by the thread
 // that has just read it.
 template <typename T> __global__ void __launch_bounds__(512) rms_fwd_wide_kernel(RmsArgs a) {
@@ -347,9 +350,7 @@ template <typename T> __global__ void __launch_bounds__(512) rms_fwd_wide_kernel
     const T *res = a.res ? (const T *)a.res + row_at(a, a.sres, r) : nullptr;
     T *h = a.h ? (T *)a.h + row_at(a, a.sh, r) : nullptr;
     auto at = [&](int i) { return res ? to_f32(x[i]) + to_f32(res[i]) : to_f32(x[i]); };
-    auto weight = [&](int i) {
-      return !a.w ? 1.f : a.w16 ? to_f32(((const bf16_t *)a.w)[i]) : ((const float *)a.w)[i];
-    };
+    auto weight = [&](int i) { return weight_at(a.w, a.w16, i, 1.f); };
     float s = 0.f;
     for (int i = threadIdx.x; i < a.C; i += blockDim.x) {
       const float z = at(i) * a.unit;
@@ -413,9 +414,7 @@ template <typename T> __global__ void __launch_bounds__(512) rms_dx_wide_kernel(
     const T *dh = a.dh ? (const T *)a.dh + row_at(a, a.sdh, r) : nullptr;
     T *dx = (T *)a.dx + row_at(a, a.sdx, r);
     const float rstd = a.rstd_in[row_at(a, a.stat, r)];
-    auto weight = [&](int i) {
-      return !a.w ? 1.f : a.w16 ? to_f32(((const bf16_t *)a.w)[i]) : ((const float *)a.w)[i];
-    };
+    auto weight = [&](int i) { return weight_at(a.w, a.w16, i, 1.f); };
     float s = 0.f;
     for (int i = threadIdx.x; i < a.C; i += blockDim.x)
       s = __builtin_fmaf(to_f32(dy[i]) * weight(i), to_f32(h[i]) * rstd, s);
@@ -442,11 +441,12 @@ template <typename T> __global__ void __launch_bounds__(512) rms_dw_wide_kernel(
 }
 
 // Inputs of 128 MB and more are read past the caches' order (the last-level one holds 256
-// MB). With it and with ordinary reads, us, inputs and outputs of three calls in turn: 16384 rows
-// of 4096 to 8 bits, 268 MB, 84 and 85 (77 and 86 where the outputs take the place of the
-// call's before); 8192 rows of 4096, 134 MB, 43 and 48, backward, 201 MB, 49 and 56; backward
-// of 65536 rows of 768 70 and 80; but 4096 rows of 4096, 67 MB, that are there from the
-// call before, 23 and 20. Pieces of 16 bytes only.
+// MB). With it and with ordinary reads, us, inputs and outputs of three calls in turn, and (in
+// brackets) where the outputs take the place of the call's before, bf16: 16384 rows of 4096
+// with a residual to 8 bits, 268 MB, 84 and 85 (75 and 85); 8192 rows, 134 MB, 43 and 45 (40 and
+// 40), to bf16 48 and 48 (43 and 43), backward, 201 MB, 49 and 55 (49 and 50); backward of 65536
+// rows of 768, 201 MB, 60 and 61 (54 and 56), of 32768 with dh, 151 MB, 39 and 44 (39 and 40);
+// but 4096 rows of 4096, 67 MB, 24 and 26 (24 and 21). Pieces of 16 bytes only.
 template <typename T, int VE> bool read_once(const RmsArgs &a, int tensors) {
   return VE * sizeof(T) == 16 && (int64_t)tensors * a.rows * a.C * (int64_t)sizeof(T) >= (int64_t)1 << 27;
 }

@@ -101,8 +101,8 @@ __device__ __forceinline__ void turn(float &u, float &v, float sn, float cs) {
   v = __builtin_fmaf(z, cs, y * sn);
 }
 
-// Thread x of the grid takes piece x % items of token x / items, of the heads that
-// blockIdx.y gives it. Items below `turning` turn: V pairs of two pieces V long and
+// Thread x of its part of the heads takes piece x % items of token x / items; workgroups
+// are the parts of the same tokens, then those of the next. Items below `turning` turn: V pairs of two pieces V long and
 // rot / 2 apart, or (IL) the V / 2 pairs of one piece (V = 1: of two elements). The
 // others are V elements that are copied.
 template <typename T, int V, bool IL, bool ONCE> __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
@@ -179,7 +179,10 @@ template <typename T, int V, bool IL, bool ONCE> __global__ void __launch_bounds
 }
 
 // The largest of 16 bytes, two elements and one that every piece of both tensors is
-// aligned to.
+// aligned to, those that are copied as those that turn. 8192 tokens of 32 heads, bf16, us, and
+// their bytes at 6.2 TB/s: d = 256, 16 bytes 51 (43), with 66 elements that turn, one by one,
+// 92; d = 250, one by one 67 (42); d = 96 25.9 (16), with 24, by two elements, 27.6; d = 80
+// 20.2 (13.5), with 20, by two, 22.2.
 int rope_vector(const mita_rope_cfg_t &c, const Strided *t, const void *const *p) {
   const int e = (int)elem_bytes(c), full = 16 / e;
   auto fits = [&](int v) {
@@ -196,10 +199,11 @@ int rope_vector(const mita_rope_cfg_t &c, const Strided *t, const void *const *p
 }
 
 // once: inputs of 128 MB and more are read past the caches' order, as in the RMS norm. With it
-// and with ordinary reads, us, inputs and outputs of three calls in turn: 4 x 8192 tokens
-// of 32 heads, d = 128, 268 MB, heads before tokens 99 and 102, tokens before heads 94 and 96;
-// 4 x 4096, 134 MB, 46 and 52; 32768 tokens of 32 + 8 heads 119 and 118; but 26 MB that
-// are there from the call before 14 and 10.
+// and with ordinary reads, us, inputs and outputs of three calls in turn, and (in brackets) where
+// the outputs take the place of the call's before: 4 x 8192 tokens of 32 heads, d = 128, 268
+// MB, heads before tokens 98 and 102 (82 and 103), tokens before heads 93 to 96 and 95 (83 and
+// 95); 4 x 4096, 134 MB, 54 and 56 (45 and 47), 51 and 51 (46 and 47); 32768 tokens of 32 + 8
+// heads 118 and 117 (116 and 117); but 3277 tokens of 32 heads, 27 MB, 13 and 11.
 template <typename T, int V> hipError_t rope_v(const RopeArgs &a, bool il, bool once, dim3 grid, hipStream_t st) {
   constexpr bool WHOLE = V * sizeof(T) == 16;
   if (il && once)
