@@ -90,3 +90,20 @@ def test_codes_of_rows_at_any_alignment(off):
     codes, scales, _ = expected(w, 128)
     y, s, _, _ = mita.rms_forward(cfg, x, w.cuda())
     assert torch.equal(s.cpu(), scales.expand(5, -1)) and torch.equal(y.view(torch.uint8).cpu(), codes.expand(5, -1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("off", [0, 1])
+@pytest.mark.parametrize("C", [1024, 32768])
+def test_a_group_past_fp32(C, off):
+    # one y beyond the largest fp32 number: its group's scale is infinite and its codes 0, but for its own, NaN
+    x = torch.ones((3, C + 8), device="cuda", dtype=torch.bfloat16)[:, off:off + C]
+    x[:, 300] = 2.0
+    w = weights(C, 128, 12)
+    w[300] = 3e38
+    y, s, _, _ = mita.rms_forward(mita.RmsConfig((3,), C, out="e4m3", group=128, eps=1e-30), x, w.cuda())
+    y = y.float().cpu()
+    assert torch.isinf(s[:, 2]).all() and torch.isfinite(s[:, :2]).all() and torch.isfinite(s[:, 3:]).all()
+    assert torch.isnan(y[:, 300]).all()
+    assert (y[:, 256:300] == 0).all() and (y[:, 301:384] == 0).all()
+    assert torch.isfinite(y[:, :256]).all() and torch.isfinite(y[:, 384:]).all()
